@@ -373,6 +373,123 @@ smat_status smat_decode_begin_gated(const smat_plan* plan, const void* K, const 
 smat_status smat_decode_step_gated(const smat_plan* plan, const void* q, const void* k, const void* v, const float* log_a_t,
                                    int64_t t, void* o, void* cache, size_t cache_bytes, void* cuda_stream);
 
+/* ---- Decode cache with its type table in 8 bits (Sec. "Memory-efficient decoding": the B type states are nearly all of it) ----
+ * A row U_h[i, :] of d_v entries is kept as int8 codes and one fp32 unit: with m = 127 / max_j |U_h[i, j]| cut to eight
+ * significant bits (at most 2^126), code = U m rounded to the nearest whole number (even between two), value = code * unit,
+ * unit = 1 / m (no larger than the element type's largest number).  A row of zeros has unit 0; a row with an entry that is not finite has unit NaN (all of its values are NaN).
+ *
+ * packed: device memory owned by the caller, 256-byte aligned, smat_decode_packed_bytes(plan) bytes: the codes
+ *        [B*H][B][d_k][d_v] int8, the units [B*H][B][d_k] fp32, then S and (gated plans) log g as in the decode cache; each
+ *        part begins at a multiple of 256 bytes.
+ * smat_decode_pack   : packs a decode cache of this plan (at any token: S and log g are copied as they are).
+ * smat_decode_unpack : the other way; values rounded to the cache's element type.
+ *        `cache` and `packed` must not overlap.
+ * smat_decode_begin_packed : smat_decode_begin (log_a NULL) or smat_decode_begin_gated (log_a given; gated plans) straight
+ *        into `packed`: equal to those followed by smat_decode_pack, without the cache between them.
+ * smat_decode_step_packed  : smat_decode_step (log_a_t NULL) or smat_decode_step_gated on `packed`.
+ * All launch on the given stream and return without synchronising; errors as for smat_decode_begin / smat_decode_step. */
+size_t smat_decode_packed_bytes(const smat_plan* plan);
+smat_status smat_decode_pack(const smat_plan* plan, const void* cache, size_t cache_bytes, void* packed, size_t packed_bytes,
+                             void* cuda_stream);
+smat_status smat_decode_unpack(const smat_plan* plan, const void* packed, size_t packed_bytes, void* cache, size_t cache_bytes,
+                               void* cuda_stream);
+smat_status smat_decode_begin_packed(const smat_plan* plan, const void* K, const void* V, const float* log_a, void* packed,
+                                     size_t packed_bytes, void* workspace, size_t workspace_bytes, void* cuda_stream);
+smat_status smat_decode_step_packed(const smat_plan* plan, const void* q, const void* k, const void* v, const float* log_a_t,
+                                    int64_t t, void* o, void* packed, size_t packed_bytes, void* cuda_stream);
+
+/* ---- Operators around the pass (the paper has no counterpart: they are what a layer has next to the pass) ----
+ * They need no plan.  Their tensors are rows of contiguous features at any stride, so that they read what a projection
+ * left and write what the pass takes (or the other way round) without a copy between.  Inputs may be broadcast (stride 0).  An output
+ * is refused (SMAT_ERR_SHAPE) where its rows overlap one another.  Pointers need the alignment of their elements; rows whose
+ * pointers, strides and widths are whole multiples of 16 bytes move in 16-byte pieces, others an element at a time.
+ * Device memory of an output may be that of an input where stated (same pointer, same strides), and must not overlap one
+ * otherwise.  The calls launch on the given stream of the current device and return without synchronising; they keep no
+ * state, and calls on several streams may run at the same time. */
+typedef struct {
+  void* data;                     /* DEVICE; inputs are not written */
+  int64_t batch, head, token;     /* strides in elements */
+} smat_rows;
+
+/* Rotary positions of Q and K.  In the first `rotated` columns of every row the pairs (x_i, x_{i + rotated/2}), or with
+ * `interleaved` the pairs (x_2i, x_2i+1), are multiplied by `scale` and turned by position * frequencies[i] radians; with `adjoint`
+ * by the negative angle (the gradient of the same call: dq from the gradient at q's output).  The other columns are copied.
+ * Angles are formed and reduced in fp64, whatever the position.
+ * q [batch, q_heads, T, d], k [batch, k_heads, T, d] (NULL: q alone).  1 <= d <= 512, rotated even, 2 <= rotated <= d.
+ * positions: NULL (token t is at first + t) or DEVICE int64, token t of sequence b at positions[b * positions_batch + t].
+ * frequencies: DEVICE fp64 [rotated / 2].  batch * T < 2^31.  An output may be its input. */
+typedef struct {
+  int batch, q_heads, k_heads;
+  int64_t T;
+  int d, rotated;
+  int interleaved, adjoint;
+  float scale;
+  smat_dtype dtype;
+  const double* frequencies;
+  const int64_t* positions;
+  int64_t positions_batch, first;
+} smat_rotary_problem;
+smat_status smat_rotary(const smat_rotary_problem* problem, const smat_rows* q, const smat_rows* k, const smat_rows* q_out,
+                        const smat_rows* k_out, void* cuda_stream);
+
+/* Root-mean-square norm of rows of `width` features, before a block or behind it; rows are indexed [batch, T, groups]
+ * (the head stride of a smat_rows steps over groups; groups = 1 for rows of a whole model):
+ *     h = residual + scale * x            (residual NULL: 0; scale NULL: 1)
+ *     y = h / sqrt(mean(h^2) + eps) * weight * act(gate)          (gate NULL: 1)
+ * weight: DEVICE fp32 [width], or [groups, width] with weight_group = width; scale: DEVICE fp32 [width].
+ * h (NULL: not kept) is stored rounded to dtype; y is formed from the unrounded rows.  h may be residual or x, y may be x or gate.
+ * Sums are fp32.  1 <= width <= 16384, groups <= 65535, batch * T < 2^31.
+ * Backward: from dy, the h that was kept (x itself where there is neither residual nor scale) and dh_in (the gradient that
+ * reaches h by other ways, NULL: none)
+ *     dh     the gradient at h, which is also that of the residual        (may be dy or dh_in)
+ *     dx     scale * dh        (NULL unless scale is given; may be dy, or x)
+ *     dgate  the gradient at the gate  (NULL unless gate is given; may be gate)
+ *     dweight [like weight], dscale [width]: fp32, summed over rows in a fixed order (the same from run to run); NULL: not wanted;
+ *            dscale needs x.
+ * workspace: DEVICE, 256-byte aligned, smat_norm_workspace_bytes(problem) bytes (only where dweight or dscale is wanted). */
+typedef enum { SMAT_ACT_SILU = 0, SMAT_ACT_SIGMOID = 1 } smat_activation;
+typedef struct {
+  int batch;
+  int64_t T;
+  int groups, width;
+  smat_dtype dtype;
+  smat_activation activation;
+  float eps;
+  const float* weight;
+  int64_t weight_group;   /* 0 or width */
+  const float* scale;
+} smat_norm_problem;
+smat_status smat_norm_forward(const smat_norm_problem* problem, const smat_rows* x, const smat_rows* residual,
+                              const smat_rows* gate, const smat_rows* y, const smat_rows* h, void* cuda_stream);
+size_t smat_norm_workspace_bytes(const smat_norm_problem* problem);
+smat_status smat_norm_backward(const smat_norm_problem* problem, const smat_rows* dy, const smat_rows* h, const smat_rows* gate,
+                               const smat_rows* x, const smat_rows* dh_in, const smat_rows* dh, const smat_rows* dx,
+                               const smat_rows* dgate, float* dweight, float* dscale, void* workspace, size_t workspace_bytes,
+                               void* cuda_stream);
+
+/* Gated linear recurrence of every channel (the vector counterpart of the scalar-gated pass, whose state is a matrix):
+ *     h_t = exp(log_a_t) h_{t-1} + x_t,   h_{-1} = h0 (NULL: 0),   t = 0 .. T-1
+ * x, log_a, h [batch, T, channels] (the head strides are not used); h0, hT [batch, channels] DEVICE fp32, contiguous: hT
+ * (NULL: not wanted) receives h_{T-1}, unrounded, and may be h0, so that T = 1 is a decoding step.  log-gates <= 0 as in
+ * smat_forward_gated, in gate_dtype (that of x, or fp32).  A closed gate (log_a = -inf) forgets all of what came before, values
+ * that are not finite among it: with one at the first token of every sequence, packed sequences do not see one another.
+ * The state is fp32.  h may be x.
+ * Backward: from dh (and dhT, the gradient at hT, NULL: none) and the h that was kept,
+ *     c_t = exp(log_a_t) (dh_t + c_{t+1}),  c_T = dhT;    dx_t = dh_t + c_{t+1},  dlog_a_t = c_t h_{t-1},  dh0 = c_0
+ * dx like x (may be dh), dlog_a like log_a (may be log_a), dh0 fp32 (NULL: not wanted; may be dhT).
+ * batch, T, channels >= 1; batch <= 65535. */
+typedef struct {
+  int batch;
+  int64_t T;
+  int channels;
+  smat_dtype dtype, gate_dtype;
+} smat_recurrence_problem;
+smat_status smat_recurrence_forward(const smat_recurrence_problem* problem, const smat_rows* x, const smat_rows* log_a,
+                                    const float* h0, const smat_rows* h, float* hT, void* cuda_stream);
+smat_status smat_recurrence_backward(const smat_recurrence_problem* problem, const smat_rows* log_a, const smat_rows* h,
+                                     const smat_rows* dh, const float* h0, const float* dhT, const smat_rows* dx,
+                                     const smat_rows* dlog_a, float* dh0, void* cuda_stream);
+
 /* Host-only self-check (the paper has no counterpart): 1 when, for field size q, every stage of the tensor-core
  * tabulation (d = 3 and 4 in both directions; d = 3 forward from q = 19 on) has a kernel whose shared-memory map (ring
  * slots, extra-class rows, output-row table, masks, barrier words) is disjoint and inside the allocation, and no load box

@@ -1,5 +1,6 @@
-"""Thin binding of libsmat.so: argument marshalling only, same names as the C boundary.  The passes and the decoding
-steps go through the native extension _smat_torch (checks, output allocation, launch), everything else through ctypes.
+"""Thin binding of libsmat.so: argument marshalling only, same names as the C boundary.  The passes, the decoding
+steps and the operators around the pass go through the native extension _smat_torch (checks, output allocation, launch),
+everything else through ctypes.
 
 Every step of the path runs inside the library's CUDA kernels.  PyTorch is used for device
 memory and streams.  There is no CPU fallback: if the shared library is missing or the device
@@ -8,6 +9,7 @@ is absent the calls raise.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -36,6 +38,9 @@ EXPORTS = [
     "smat_static_check_status", "smat_debug_timeout_probe", "smat_measure_fadd_rate",
     "smat_forward_routed", "smat_backward_routed", "smat_forward_gated", "smat_backward_gated",
     "smat_forward_normalized", "smat_backward_normalized", "smat_debug_tabulation_layout_ok",
+    "smat_decode_packed_bytes", "smat_decode_pack", "smat_decode_unpack", "smat_decode_begin_packed", "smat_decode_step_packed",
+    "smat_rotary", "smat_norm_forward", "smat_norm_workspace_bytes", "smat_norm_backward",
+    "smat_recurrence_forward", "smat_recurrence_backward",
 ]
 
 
@@ -49,6 +54,29 @@ class _Geometry(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int64), ("c", ctypes.c_int64), ("n", ctypes.c_int64), ("m", ctypes.c_int64),
                 ("d", ctypes.c_int32), ("q", ctypes.c_int32), ("P", ctypes.c_int64), ("A", ctypes.c_int64),
                 ("B", ctypes.c_int64), ("nnzC", ctypes.c_int64), ("vc_conditions_met", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    """smat_rows: rows of contiguous features, strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class RotaryProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("q_heads", ctypes.c_int), ("k_heads", ctypes.c_int), ("T", ctypes.c_int64),
+                ("d", ctypes.c_int), ("rotated", ctypes.c_int), ("interleaved", ctypes.c_int), ("adjoint", ctypes.c_int),
+                ("scale", ctypes.c_float), ("dtype", ctypes.c_int), ("frequencies", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_batch", ctypes.c_int64), ("first", ctypes.c_int64)]
+
+
+class NormProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("T", ctypes.c_int64), ("groups", ctypes.c_int), ("width", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("activation", ctypes.c_int), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p),
+                ("weight_group", ctypes.c_int64), ("scale", ctypes.c_void_p)]
+
+
+class RecurrenceProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("T", ctypes.c_int64), ("channels", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("gate_dtype", ctypes.c_int)]
 
 
 @dataclass(frozen=True)
@@ -126,6 +154,29 @@ def load_library() -> ctypes.CDLL:
     lib.smat_decode_begin_gated.restype = i
     lib.smat_decode_step_gated.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, ctypes.c_size_t, vp]
     lib.smat_decode_step_gated.restype = i
+    lib.smat_decode_packed_bytes.argtypes = [vp]
+    lib.smat_decode_packed_bytes.restype = ctypes.c_size_t
+    lib.smat_decode_pack.argtypes = [vp, vp, sz, vp, sz, vp]
+    lib.smat_decode_pack.restype = i
+    lib.smat_decode_unpack.argtypes = [vp, vp, sz, vp, sz, vp]
+    lib.smat_decode_unpack.restype = i
+    lib.smat_decode_begin_packed.argtypes = [vp, vp, vp, vp, vp, sz, vp, sz, vp]
+    lib.smat_decode_begin_packed.restype = i
+    lib.smat_decode_step_packed.argtypes = [vp, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+    lib.smat_decode_step_packed.restype = i
+    rows = [ctypes.POINTER(Rows)]
+    lib.smat_rotary.argtypes = [ctypes.POINTER(RotaryProblem)] + rows * 4 + [vp]
+    lib.smat_rotary.restype = i
+    lib.smat_norm_forward.argtypes = [ctypes.POINTER(NormProblem)] + rows * 5 + [vp]
+    lib.smat_norm_forward.restype = i
+    lib.smat_norm_workspace_bytes.argtypes = [ctypes.POINTER(NormProblem)]
+    lib.smat_norm_workspace_bytes.restype = sz
+    lib.smat_norm_backward.argtypes = [ctypes.POINTER(NormProblem)] + rows * 8 + [vp, vp, vp, sz, vp]
+    lib.smat_norm_backward.restype = i
+    lib.smat_recurrence_forward.argtypes = [ctypes.POINTER(RecurrenceProblem)] + rows * 2 + [vp] + rows + [vp, vp]
+    lib.smat_recurrence_forward.restype = i
+    lib.smat_recurrence_backward.argtypes = [ctypes.POINTER(RecurrenceProblem)] + rows * 3 + [vp, vp] + rows * 2 + [vp, vp]
+    lib.smat_recurrence_backward.restype = i
     lib.smat_profile_table_element_bytes.argtypes = [vp]
     lib.smat_profile_table_element_bytes.restype = i
     lib.smat_uses_tensor_cores.argtypes = [vp]
@@ -226,6 +277,93 @@ def measure_fadd_rate(packed: bool = False, stream=None) -> float:
     _check(load_library().smat_measure_fadd_rate(_ptr(scratch), int(packed), ctypes.byref(out), _stream(stream)),
            "smat_measure_fadd_rate")
     return float(out.value)
+
+
+# -- operators around the pass ---------------------------------------------------------------------
+def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0, trained_length: int = 4096,
+                       fast_turns: float = 32.0, slow_turns: float = 1.0, device="cuda"):
+    """(frequencies, scale) for rotary(): radians a token of every pair, base ** (-2 i / rotated), as an fp64 tensor, and the
+    factor on the rotated columns.
+
+    scaling stretches a model's context by `factor`: "linear" divides every frequency by it; "ntk" raises the base so that the
+    slowest pair is stretched by it and the fastest stays; "yarn" divides the frequencies of pairs that turn less than
+    `slow_turns` times in `trained_length` tokens, keeps those of pairs that turn more than `fast_turns` times, blends between
+    them, and scales by 0.1 ln(factor) + 1."""
+    if rotated < 2 or rotated % 2:
+        raise ValueError("rotated: expected an even number of columns")
+    if scaling not in (None, "linear", "ntk", "yarn"):
+        raise ValueError("scaling: expected None, 'linear', 'ntk' or 'yarn'")
+    if not (base > 1.0 and factor >= 1.0):
+        raise ValueError("expected base > 1 and factor >= 1")
+    if scaling == "ntk" and rotated > 2:
+        base = base * factor ** (rotated / (rotated - 2))
+    f = base ** (-torch.arange(0, rotated, 2, dtype=torch.float64) / rotated)
+    scale = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        if trained_length < 1 or not fast_turns > slow_turns > 0.0:
+            raise ValueError("yarn: expected trained_length >= 1 and fast_turns > slow_turns > 0")
+        pair = [rotated * math.log(trained_length / (turns * 2.0 * math.pi)) / (2.0 * math.log(base)) for turns in (fast_turns, slow_turns)]
+        lo, hi = max(math.floor(pair[0]), 0), min(math.ceil(pair[1]), rotated - 1)
+        stretched = ((torch.arange(rotated // 2, dtype=torch.float64) - lo) / max(hi - lo, 1e-3)).clamp(0.0, 1.0)
+        f = f * (1.0 - stretched) + f / factor * stretched
+        scale = 0.1 * math.log(factor) + 1.0
+    return f.to(device), scale
+
+
+def rotary(Q, K, frequencies, positions=None, first: int = 0, interleaved: bool = False, scale: float = 1.0, adjoint: bool = False,
+           Q_out=None, K_out=None, stream=None):
+    """smat_rotary: Q, K [batch, heads, T, d] (any strides; K may be None, or have another number of heads) or rows of single tokens
+    [batch, heads, d], turned by their positions; new contiguous tensors, as SmatPlan takes them, unless outputs are given.
+
+    frequencies: fp64 [rotated / 2] (see rotary_frequencies).  positions: int64 [T] or [batch, T] (single tokens: also [batch]), on
+    the device; without them token t is at first + t.  adjoint: turned back, the gradient of the same call."""
+    return _extension().rotary(Q, K, frequencies, positions, first, interleaved, scale, adjoint, Q_out, K_out, stream)
+
+
+def _sigmoid(activation: str) -> bool:
+    if activation not in ("silu", "sigmoid"):
+        raise ValueError("activation: expected 'silu' or 'sigmoid'")
+    return activation == "sigmoid"
+
+
+def norm_forward(X, weight, eps: float = 1e-6, residual=None, scale=None, gate=None, activation: str = "silu", Y=None, H=None, stream=None):
+    """smat_norm_forward: Y = h / sqrt(mean(h^2) + eps) * weight * act(gate) with h = residual + scale * X, over the last dimension
+    of X [batch, T, groups, width], [batch, T, width] or [rows, width] (any strides).
+
+    weight: fp32 [width], or [groups, width] (then also X [batch, groups, width], single tokens).  scale: fp32 [width].  Returns Y;
+    with a residual, a scale or an H to write also h in X's type: (Y, H)."""
+    return _extension().norm_forward(X, weight, eps, residual, scale, gate, _sigmoid(activation), Y, H, stream)
+
+
+def norm_backward(dY, H, weight, eps: float = 1e-6, gate=None, activation: str = "silu", dH=None, X=None, scale=None, dH_out=None, dX=None,
+                  dgate=None, workspace=None, stream=None):
+    """smat_norm_backward: (dH, dX, dweight, dscale, dgate) from dY, the H that the forward returned (X where it returned none) and
+    the gradient dH that reaches h by other ways.
+
+    dH is the residual's gradient too; without a scale dX is dH itself; dscale and dgate are None without a scale (which needs X) or
+    a gate.  dweight, dscale: fp32.  dH_out, dX, dgate: outputs to write.  workspace: uint8, norm_workspace_bytes(...) of them."""
+    return _extension().norm_backward(dY, H, weight, eps, gate, _sigmoid(activation), dH, X, scale, dH_out, dX, dgate, workspace, stream)
+
+
+def norm_workspace_bytes(width: int, groups: int = 1, scale: bool = False) -> int:
+    """smat_norm_workspace_bytes: what norm_backward needs for rows of this width, with or without a scale."""
+    p = NormProblem(batch=1, T=1, groups=groups, width=width, dtype=SMAT_F32, weight=256, scale=256 if scale else None)
+    return int(load_library().smat_norm_workspace_bytes(ctypes.byref(p)))
+
+
+def recurrence_forward(X, log_a, h0=None, H=None, hT=None, stream=None):
+    """smat_recurrence_forward: (H, hT), h_t = exp(log_a_t) h_{t-1} + x_t for every channel of X, log_a [batch, T, channels] (any
+    strides) or [batch, channels], one token.
+
+    log_a in X's type or fp32; h0, hT fp32 [batch, channels]; for decoding steps hT may be h0, updated in place."""
+    return _extension().recurrence_forward(X, log_a, h0, H, hT, stream)
+
+
+def recurrence_backward(log_a, H, dH, h0=None, dhT=None, dX=None, dlog_a=None, dh0=None, stream=None):
+    """smat_recurrence_backward: (dX, dlog_a, dh0) from the H that the forward returned, the gradients at H and (dhT) at hT."""
+    return _extension().recurrence_backward(log_a, H, dH, h0, dhT, dX, dlog_a, dh0, stream)
 
 
 class SmatPlan:
@@ -354,7 +492,7 @@ class SmatPlan:
                                           _stream(stream)), "smat_decode_begin")
 
     def decode_step(self, q, k, v, t: int, cache, o=None, stream=None):
-        return self._native.decode_step(q, k, v, None, t, cache, o, stream)
+        return self._native.decode_step(q, k, v, None, t, cache, o, stream, False)
 
     def decode_begin_gated(self, K, V, log_a, cache, workspace=None, stream=None) -> None:
         _, _, _, dk, dv = self.shape
@@ -368,7 +506,50 @@ class SmatPlan:
     def decode_step_gated(self, q, k, v, log_a_t, t: int, cache, o=None, stream=None):
         if log_a_t is None:
             raise ValueError("log_a_t: expected the log-gates of token t")
-        return self._native.decode_step(q, k, v, log_a_t, t, cache, o, stream)
+        return self._native.decode_step(q, k, v, log_a_t, t, cache, o, stream, False)
+
+    # -- cached decoding with the type table in 8 bits ---------------------------------------------
+    def decode_cache_packed(self, device="cuda") -> torch.Tensor:
+        return torch.empty(int(self.lib.smat_decode_packed_bytes(self.handle)), dtype=torch.uint8, device=device)
+
+    def decode_pack(self, cache, packed=None, stream=None) -> torch.Tensor:
+        """smat_decode_pack: the packed form of a decode cache."""
+        self._check_bytes(cache, "cache")
+        packed = self.decode_cache_packed(cache.device) if packed is None else packed
+        self._check_bytes(packed, "packed")
+        _check(self.lib.smat_decode_pack(self.handle, _ptr(cache), cache.numel(), _ptr(packed), packed.numel(), _stream(stream)),
+               "smat_decode_pack")
+        return packed
+
+    def decode_unpack(self, packed, cache=None, stream=None) -> torch.Tensor:
+        """smat_decode_unpack: the decode cache that a packed one stands for."""
+        self._check_bytes(packed, "packed")
+        cache = self.decode_cache(packed.device) if cache is None else cache
+        self._check_bytes(cache, "cache")
+        _check(self.lib.smat_decode_unpack(self.handle, _ptr(packed), packed.numel(), _ptr(cache), cache.numel(), _stream(stream)),
+               "smat_decode_unpack")
+        return cache
+
+    def decode_begin_packed(self, K, V, packed, log_a=None, workspace=None, stream=None) -> None:
+        """smat_decode_begin_packed; log_a [batch*heads, T] on gated plans."""
+        _, _, _, dk, dv = self.shape
+        self._check_tensor(K, dk, "K"); self._check_tensor(V, dv, "V")
+        self._check_bytes(packed, "packed")
+        if log_a is not None:
+            self._check_gates(log_a)
+        ws = self.workspace(False, K.device) if workspace is None else workspace
+        self._ws = ws
+        _check(self.lib.smat_decode_begin_packed(self.handle, _ptr(K), _ptr(V), _ptr(log_a), _ptr(packed), packed.numel(), _ptr(ws),
+                                                 ws.numel(), _stream(stream)), "smat_decode_begin_packed")
+
+    def decode_step_packed(self, q, k, v, t: int, packed, log_a_t=None, o=None, stream=None):
+        """smat_decode_step_packed; log_a_t, the token's log-gates, on gated plans."""
+        return self._native.decode_step(q, k, v, log_a_t, t, packed, o, stream, True)
+
+    @staticmethod
+    def _check_bytes(t: torch.Tensor, name: str) -> None:
+        if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()):
+            raise ValueError(f"{name}: expected a contiguous CUDA uint8 tensor")
 
     # -- verification exports ------------------------------------------------------------------
     def routing_indices(self):

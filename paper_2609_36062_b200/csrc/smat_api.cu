@@ -519,6 +519,22 @@ size_t decode_table_bytes(const smat_plan* pl) {
   return align_up((size_t)pl->bh * pl->geo.B * pl->rp * (decode_table_plan(pl)->u_bf16 ? 2 : 4));
 }
 size_t decode_state_bytes(const smat_plan* pl) { return align_up((size_t)pl->bh * pl->rp * sizeof(float)); }
+// What a decode cache and a packed one have behind the type table: running states, and on gated plans the log-gates.
+size_t decode_tail_bytes(const smat_plan* pl) {
+  return decode_state_bytes(pl) + ((pl->flags & SMAT_FLAG_GATED) ? align_up((size_t)pl->bh * 4) : 0);
+}
+int64_t decode_rows(const smat_plan* pl) { return (int64_t)pl->bh * pl->geo.B * pl->r; }
+size_t decode_codes_bytes(const smat_plan* pl) { return align_up((size_t)decode_rows(pl) * pl->p); }
+size_t decode_units_bytes(const smat_plan* pl) { return align_up((size_t)decode_rows(pl) * sizeof(float)); }
+struct PackedCache {
+  char* codes;
+  float* units;
+  char* tail;      // S, then log g
+};
+PackedCache packed_cache(const smat_plan* pl, void* packed) {
+  char* base = static_cast<char*>(packed);
+  return {base, reinterpret_cast<float*>(base + decode_codes_bytes(pl)), base + decode_codes_bytes(pl) + decode_units_bytes(pl)};
+}
 
 }  // namespace
 
@@ -1174,6 +1190,60 @@ smat_status gated_check(const smat_plan* pl, const void* log_a, void* ws, size_t
   return SMAT_OK;
 }
 
+// The type table that a decode cache begins with, formed in the workspace (steps 2-3 of Algorithm 1).  Gated (log_a given): from λ
+// and the keys rescaled to the block boundary (rows t < n of the split copy).
+struct DecodeTable {
+  const char* data;
+  size_t bytes;
+  int bf16;
+};
+DecodeTable decode_table(Ctx& cx, const void* K, const void* V, const float* log_a) {
+  const smat_plan *pl = cx.pl, *tp = decode_table_plan(pl);
+  pl->stages = 0;
+  cx.err = clear_status(cx);
+  DecodeTable t{nullptr, (size_t)pl->bh * pl->geo.B * pl->rp * (tp->u_bf16 ? 2 : 4), tp->u_bf16 ? 1 : 0};
+  if (!log_a) {
+    t.data = cx.ws + build_type_table(cx, K, V);
+    return t;
+  }
+  const Gated gt = gated_buffers(cx);
+  SMAT_TRY(cx, "gate_prefix", smat_launch_head_scan(log_a, gt.lam, pl->T, pl->bh, 0, cx.st));
+  gate_scale(cx, "gate_scale_lr", K, K, gt.lr, gt.lam, 2, pl->r);
+  Ctx ct{tp, cx.st, cx.ws + (tp == pl ? 0 : pl->off_inner), cx.err, 0};
+  ct.rec = pl;
+  t.data = ct.ws + build_type_table(ct, gt.lr, V);
+  cx.err = ct.err;
+  cx.launches += ct.launches;
+  return t;
+}
+
+smat_status decode_begin_ready(const void* K, const void* V, const void* cache, size_t cache_bytes, size_t need) {
+  if (cache_bytes < need) return SMAT_ERR_WORKSPACE;
+  if (misaligned(K) || misaligned(V) || (reinterpret_cast<uintptr_t>(cache) & 255)) return SMAT_ERR_ALIGN;
+  return device_ok() ? SMAT_OK : SMAT_ERR_ARCH;
+}
+
+smat_status packing_check(const smat_plan* pl, const void* cache, size_t cache_bytes, const void* packed, size_t packed_bytes) {
+  if (!pl || !cache || !packed) return SMAT_ERR_NULL;
+  if (cache_bytes < smat_decode_cache_bytes(pl) || packed_bytes < smat_decode_packed_bytes(pl)) return SMAT_ERR_WORKSPACE;
+  if (smat_overlap(cache, smat_decode_cache_bytes(pl), packed, smat_decode_packed_bytes(pl))) return SMAT_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(cache) | reinterpret_cast<uintptr_t>(packed)) & 255) return SMAT_ERR_ALIGN;
+  return device_ok() ? SMAT_OK : SMAT_ERR_ARCH;
+}
+
+smat_status decode_begin(const smat_plan* pl, const void* K, const void* V, const float* log_a, void* cache, size_t cache_bytes,
+                         void* workspace, void* cuda_stream) {
+  const smat_status s = decode_begin_ready(K, V, cache, cache_bytes, smat_decode_cache_bytes(pl));
+  if (s != SMAT_OK) return s;
+  Ctx cx{pl, static_cast<cudaStream_t>(cuda_stream), static_cast<char*>(workspace), cudaSuccess, 0};
+  const DecodeTable t = decode_table(cx, K, V, log_a);
+  if (cx.err == cudaSuccess) cx.err = cudaMemcpyAsync(cache, t.data, t.bytes, cudaMemcpyDeviceToDevice, cx.st);
+  if (cx.err == cudaSuccess)   // S = 0 and log g = 0 (they follow the table)
+    cx.err = cudaMemsetAsync(static_cast<char*>(cache) + decode_table_bytes(pl), 0, decode_tail_bytes(pl), cx.st);
+  pl->launches = cx.launches;
+  return cx.err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1461,30 +1531,16 @@ int smat_debug_tabulation_layout_ok(int q) { return smat_tabulate_tc_layout_ok(q
 
 size_t smat_decode_cache_bytes(const smat_plan* pl) {
   if (!pl) return 0;   // type table, running state, and on gated plans the running log-gate of every head
-  return decode_table_bytes(pl) + decode_state_bytes(pl) + ((pl->flags & SMAT_FLAG_GATED) ? align_up((size_t)pl->bh * 4) : 0);
+  return decode_table_bytes(pl) + decode_tail_bytes(pl);
 }
 
 smat_status smat_decode_begin(const smat_plan* pl, const void* K, const void* V, void* cache, size_t cache_bytes,
                               void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (!K || !V || !cache) return SMAT_ERR_NULL;
   if (pl && (pl->flags & SMAT_FLAG_GATED)) return SMAT_ERR_UNSUPPORTED;   // gated plans decode with the gated pair of calls
-  smat_status s = check_common(pl, workspace, workspace_bytes, 0);
+  const smat_status s = check_common(pl, workspace, workspace_bytes, 0);
   if (s != SMAT_OK) return s;
-  if (cache_bytes < smat_decode_cache_bytes(pl)) return SMAT_ERR_WORKSPACE;
-  if (misaligned(K) || misaligned(V) || (reinterpret_cast<uintptr_t>(cache) & 255)) return SMAT_ERR_ALIGN;
-  if (!device_ok()) return SMAT_ERR_ARCH;
-  Ctx cx{pl, static_cast<cudaStream_t>(cuda_stream), static_cast<char*>(workspace), cudaSuccess, 0};
-  pl->stages = 0;
-  cx.err = clear_status(cx);
-  const size_t off = build_type_table(cx, K, V);
-  const size_t tbytes = (size_t)pl->bh * pl->geo.B * pl->rp * (pl->u_bf16 ? 2 : 4);
-  if (cx.err == cudaSuccess)
-    cx.err = cudaMemcpyAsync(cache, cx.ws + off, tbytes, cudaMemcpyDeviceToDevice, cx.st);
-  if (cx.err == cudaSuccess)
-    cx.err = cudaMemsetAsync(static_cast<char*>(cache) + decode_table_bytes(pl), 0, (size_t)pl->bh * pl->rp * sizeof(float),
-                             cx.st);
-  pl->launches = cx.launches;
-  return cx.err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+  return decode_begin(pl, K, V, nullptr, cache, cache_bytes, workspace, cuda_stream);
 }
 
 smat_status smat_decode_step(const smat_plan* pl, const void* q, const void* k, const void* v, int64_t t, void* o,
@@ -1506,30 +1562,9 @@ smat_status smat_decode_step(const smat_plan* pl, const void* q, const void* k, 
 smat_status smat_decode_begin_gated(const smat_plan* pl, const void* K, const void* V, const float* log_a, void* cache,
                                     size_t cache_bytes, void* workspace, size_t workspace_bytes, void* cuda_stream) {
   if (!K || !V || !cache) return SMAT_ERR_NULL;
-  smat_status s = gated_check(pl, log_a, workspace, workspace_bytes, 0);
+  const smat_status s = gated_check(pl, log_a, workspace, workspace_bytes, 0);
   if (s != SMAT_OK) return s;
-  if (cache_bytes < smat_decode_cache_bytes(pl)) return SMAT_ERR_WORKSPACE;
-  if (misaligned(K) || misaligned(V) || (reinterpret_cast<uintptr_t>(cache) & 255)) return SMAT_ERR_ALIGN;
-  if (!device_ok()) return SMAT_ERR_ARCH;
-  Ctx cx{pl, static_cast<cudaStream_t>(cuda_stream), static_cast<char*>(workspace), cudaSuccess, 0};
-  pl->stages = 0;
-  cx.err = clear_status(cx);
-  const Gated gt = gated_buffers(cx);
-  // λ, the keys rescaled to the block boundary (rows t < n of the split copy), then steps 2-3 of Algorithm 1 on them
-  SMAT_TRY(cx, "gate_prefix", smat_launch_head_scan(log_a, gt.lam, pl->T, pl->bh, 0, cx.st));
-  gate_scale(cx, "gate_scale_lr", K, K, gt.lr, gt.lam, 2, pl->r);
-  const smat_plan* tp = decode_table_plan(pl);
-  Ctx ct{tp, cx.st, cx.ws + (tp == pl ? 0 : pl->off_inner), cx.err, 0};
-  ct.rec = pl;
-  const size_t off = build_type_table(ct, gt.lr, V);
-  cx.err = ct.err;
-  const size_t tbytes = (size_t)pl->bh * pl->geo.B * pl->rp * (tp->u_bf16 ? 2 : 4);
-  if (cx.err == cudaSuccess) cx.err = cudaMemcpyAsync(cache, ct.ws + off, tbytes, cudaMemcpyDeviceToDevice, cx.st);
-  if (cx.err == cudaSuccess)   // S = 0 and log g = 0 (they follow the table)
-    cx.err = cudaMemsetAsync(static_cast<char*>(cache) + decode_table_bytes(pl), 0,
-                             smat_decode_cache_bytes(pl) - decode_table_bytes(pl), cx.st);
-  pl->launches = cx.launches + ct.launches;
-  return cx.err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+  return decode_begin(pl, K, V, log_a, cache, cache_bytes, workspace, cuda_stream);
 }
 
 smat_status smat_decode_step_gated(const smat_plan* pl, const void* q, const void* k, const void* v, const float* log_a_t,
@@ -1546,6 +1581,71 @@ smat_status smat_decode_step_gated(const smat_plan* pl, const void* q, const voi
   const cudaError_t err = smat_launch_decode_step(q, k, v, o, S, cache, decode_table_plan(pl)->u_bf16 ? 1 : 0,
                                                   pl->dtype == SMAT_BF16 ? 1 : 0, smat_type_of(pl->geo, t), pl->geo.B, pl->r,
                                                   pl->p, pl->bh, static_cast<cudaStream_t>(cuda_stream), log_a_t, log_g);
+  pl->launches = 1;
+  return err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+}
+
+size_t smat_decode_packed_bytes(const smat_plan* pl) {
+  if (!pl) return 0;
+  return decode_codes_bytes(pl) + decode_units_bytes(pl) + decode_tail_bytes(pl);
+}
+
+smat_status smat_decode_pack(const smat_plan* pl, const void* cache, size_t cache_bytes, void* packed, size_t packed_bytes,
+                             void* cuda_stream) {
+  const smat_status s = packing_check(pl, cache, cache_bytes, packed, packed_bytes);
+  if (s != SMAT_OK) return s;
+  const PackedCache to = packed_cache(pl, packed);
+  const cudaError_t err = smat_launch_pack(cache, decode_table_plan(pl)->u_bf16 ? 1 : 0, to.codes, to.units, decode_rows(pl), pl->p,
+                                           static_cast<const char*>(cache) + decode_table_bytes(pl), to.tail, decode_tail_bytes(pl),
+                                           static_cast<cudaStream_t>(cuda_stream));
+  pl->launches = 1;
+  return err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+}
+
+smat_status smat_decode_unpack(const smat_plan* pl, const void* packed, size_t packed_bytes, void* cache, size_t cache_bytes,
+                               void* cuda_stream) {
+  const smat_status s = packing_check(pl, cache, cache_bytes, packed, packed_bytes);
+  if (s != SMAT_OK) return s;
+  const PackedCache from = packed_cache(pl, const_cast<void*>(packed));
+  const cudaError_t err = smat_launch_unpack(from.codes, from.units, cache, decode_table_plan(pl)->u_bf16 ? 1 : 0, decode_rows(pl), pl->p,
+                                             from.tail, static_cast<char*>(cache) + decode_table_bytes(pl), decode_tail_bytes(pl),
+                                             static_cast<cudaStream_t>(cuda_stream));
+  pl->launches = 1;
+  return err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+}
+
+smat_status smat_decode_begin_packed(const smat_plan* pl, const void* K, const void* V, const float* log_a, void* packed,
+                                     size_t packed_bytes, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!K || !V || !packed) return SMAT_ERR_NULL;
+  if (pl && !log_a && (pl->flags & SMAT_FLAG_GATED)) return SMAT_ERR_NULL;   // a gated plan's tables need the gates
+  smat_status s = log_a ? gated_check(pl, log_a, workspace, workspace_bytes, 0) : check_common(pl, workspace, workspace_bytes, 0);
+  if (s != SMAT_OK) return s;
+  s = decode_begin_ready(K, V, packed, packed_bytes, smat_decode_packed_bytes(pl));
+  if (s != SMAT_OK) return s;
+  Ctx cx{pl, static_cast<cudaStream_t>(cuda_stream), static_cast<char*>(workspace), cudaSuccess, 0};
+  const DecodeTable t = decode_table(cx, K, V, log_a);
+  const PackedCache to = packed_cache(pl, packed);
+  SMAT_TRY(cx, "pack", smat_launch_pack(t.data, t.bf16, to.codes, to.units, decode_rows(pl), pl->p, nullptr, nullptr, 0, cx.st));
+  if (cx.err == cudaSuccess) cx.err = cudaMemsetAsync(to.tail, 0, decode_tail_bytes(pl), cx.st);
+  pl->launches = cx.launches;
+  return cx.err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
+}
+
+smat_status smat_decode_step_packed(const smat_plan* pl, const void* q, const void* k, const void* v, const float* log_a_t,
+                                    int64_t t, void* o, void* packed, size_t packed_bytes, void* cuda_stream) {
+  if (!pl || !q || !k || !v || !o || !packed) return SMAT_ERR_NULL;
+  const bool gated = (pl->flags & SMAT_FLAG_GATED) != 0;
+  if (gated && !log_a_t) return SMAT_ERR_NULL;
+  if (!gated && log_a_t) return SMAT_ERR_UNSUPPORTED;
+  if (packed_bytes < smat_decode_packed_bytes(pl)) return SMAT_ERR_WORKSPACE;
+  if (t < pl->geo.n || t >= pl->T) return SMAT_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(packed) & 255) || (reinterpret_cast<uintptr_t>(log_a_t) & 3)) return SMAT_ERR_ALIGN;
+  if (!device_ok()) return SMAT_ERR_ARCH;
+  const PackedCache c = packed_cache(pl, packed);
+  const cudaError_t err = smat_launch_decode_step_packed(q, k, v, o, reinterpret_cast<float*>(c.tail), c.codes, c.units,
+                                                         pl->dtype == SMAT_BF16 ? 1 : 0, smat_type_of(pl->geo, t), pl->geo.B, pl->r,
+                                                         pl->p, pl->bh, static_cast<cudaStream_t>(cuda_stream), log_a_t,
+                                                         gated ? reinterpret_cast<float*>(c.tail + decode_state_bytes(pl)) : nullptr);
   pl->launches = 1;
   return err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
 }

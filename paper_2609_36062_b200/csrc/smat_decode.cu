@@ -44,12 +44,20 @@ __device__ __forceinline__ float4 load_state4<__nv_bfloat16>(const __nv_bfloat16
                      __uint_as_float(w.y & 0xffff0000u));
 }
 
+template <>
+__device__ __forceinline__ float4 load_state4<int8_t>(const int8_t* p) {
+  int32_t w;
+  asm volatile("ld.global.L1::no_allocate.s32 %0, [%1];" : "=r"(w) : "l"(p));
+  return make_float4((float)(int8_t)w, (float)(int8_t)(w >> 8), (float)(int8_t)(w >> 16), (float)(w >> 24));
+}
+
 // One CTA per head and 32 columns of the state (128 bytes of a row), so that even a handful of sequences spreads over
 // the SMs.  Thread (row tid / 8, columns 4 (tid % 8)) walks the rows 32 at a time with every load of its share in
 // flight before the first use: a CTA's 24 KB are one round trip to memory.  The partial outputs meet by shuffles and
 // one row of shared memory per warp (no atomics: the sum's order is fixed).  Bound by the 84 MB a step of 512 heads
 // moves: 14.6 us (12.8 at the HBM rate; 15.7 without the prefetch), where one CTA per head with one row pass in flight at
 // a time took 22.1.
+// Packed type table (TU = int8_t): the unit of a row joins its gate factor, u = (g unit) code.
 constexpr int DEC_COLS = 32, DEC_ROWS = 32, DEC_THREADS = 256;
 
 // TOGETHER: the CTAs of a head are a cluster and none writes o or the running gate before all have read q, k and it (gated
@@ -59,7 +67,7 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
                                                           const T* v, T* o,
                                                           float* S, const TU* U, int64_t type,
                                                           int64_t types, int p, const float* log_a,
-                                                          float* log_g) {
+                                                          float* log_g, const float* units) {
   constexpr int r = PASSES * DEC_ROWS;
   __shared__ float part[DEC_THREADS / 32][DEC_COLS];
   pdl_trigger();
@@ -72,7 +80,7 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
   float* Sh = S + (int64_t)bh * r * p + j;
   const TU* Uh = Ub + j;
   float4 s[PASSES], u[PASSES];
-  float qi[PASSES], ki[PASSES];
+  float qi[PASSES], ki[PASSES], unit[PASSES];
 #pragma unroll
   for (int n = 0; n < PASSES; ++n) {
     const int64_t off = (int64_t)(n * DEC_ROWS + i0) * p;
@@ -83,6 +91,7 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
   for (int n = 0; n < PASSES; ++n) {
     qi[n] = to_f32(q[(int64_t)bh * r + n * DEC_ROWS + i0]);
     ki[n] = to_f32(k[(int64_t)bh * r + n * DEC_ROWS + i0]);
+    unit[n] = sizeof(TU) == 1 ? units[((int64_t)bh * types + type) * r + n * DEC_ROWS + i0] : 1.f;
   }
   const T* vrow = v + (int64_t)bh * p + j;
   const float v0 = to_f32(vrow[0]), v1 = to_f32(vrow[1]), v2 = to_f32(vrow[2]), v3 = to_f32(vrow[3]);
@@ -96,8 +105,9 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
     s[n].x = fmaf(ki[n], v0, a * s[n].x); s[n].y = fmaf(ki[n], v1, a * s[n].y);
     s[n].z = fmaf(ki[n], v2, a * s[n].z); s[n].w = fmaf(ki[n], v3, a * s[n].w);
     *reinterpret_cast<float4*>(Sh + (int64_t)(n * DEC_ROWS + i0) * p) = s[n];     // S_t = a_t S_{t-1} + k vᵀ
-    o4[0] = fmaf(qi[n], fmaf(g, u[n].x, s[n].x), o4[0]); o4[1] = fmaf(qi[n], fmaf(g, u[n].y, s[n].y), o4[1]);
-    o4[2] = fmaf(qi[n], fmaf(g, u[n].z, s[n].z), o4[2]); o4[3] = fmaf(qi[n], fmaf(g, u[n].w, s[n].w), o4[3]);
+    const float f = sizeof(TU) == 1 ? g * unit[n] : g;
+    o4[0] = fmaf(qi[n], fmaf(f, u[n].x, s[n].x), o4[0]); o4[1] = fmaf(qi[n], fmaf(f, u[n].y, s[n].y), o4[1]);
+    o4[2] = fmaf(qi[n], fmaf(f, u[n].z, s[n].z), o4[2]); o4[3] = fmaf(qi[n], fmaf(f, u[n].w, s[n].w), o4[3]);
   }
   if (TOGETHER) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
 #pragma unroll
@@ -119,7 +129,8 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
 
 template <typename T, typename TU>
 cudaError_t launch_step(const void* q, const void* k, const void* v, void* o, float* S, const void* U, int64_t type,
-                        int64_t types, int r, int p, int bh, cudaStream_t st, const float* log_a, float* log_g) {
+                        int64_t types, int r, int p, int bh, cudaStream_t st, const float* log_a, float* log_g,
+                        const float* units = nullptr) {
   const unsigned slices = (unsigned)(p / DEC_COLS);
   // o in the place of q or k (o in the place of v needs nothing: a CTA reads just the columns that it writes)
   const size_t in = (size_t)bh * r * sizeof(T), out = (size_t)bh * p * sizeof(T);
@@ -128,7 +139,7 @@ cudaError_t launch_step(const void* q, const void* k, const void* v, void* o, fl
                         : (together ? decode_step_kernel<T, TU, 4, true> : decode_step_kernel<T, TU, 4, false>);
   return smat_launch_pdl_cluster(kernel, dim3(slices, (unsigned)bh), DEC_THREADS, 0, together ? slices : 1u, st,
                                  static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
-                                 static_cast<T*>(o), S, static_cast<const TU*>(U), type, types, p, log_a, log_g);
+                                 static_cast<T*>(o), S, static_cast<const TU*>(U), type, types, p, log_a, log_g, units);
 }
 
 }  // namespace
@@ -143,4 +154,13 @@ cudaError_t smat_launch_decode_step(const void* q, const void* k, const void* v,
     return u_bf16 ? cudaErrorInvalidValue : launch_step<float, float>(q, k, v, o, S, U, type, types, r, p, bh, st, log_a, log_g);
   return u_bf16 ? launch_step<__nv_bfloat16, __nv_bfloat16>(q, k, v, o, S, U, type, types, r, p, bh, st, log_a, log_g)
                 : launch_step<__nv_bfloat16, float>(q, k, v, o, S, U, type, types, r, p, bh, st, log_a, log_g);
+}
+
+// The same on a packed type table: codes [bh][types][r][p] int8 and units [bh][types][r].
+cudaError_t smat_launch_decode_step_packed(const void* q, const void* k, const void* v, void* o, float* S, const void* codes,
+                                           const float* units, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
+                                           cudaStream_t st, const float* log_a, float* log_g) {
+  if ((r != 64 && r != 128) || (p != 64 && p != 128)) return cudaErrorInvalidValue;
+  return in_bf16 ? launch_step<__nv_bfloat16, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units)
+                 : launch_step<float, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units);
 }

@@ -221,6 +221,15 @@ cudaError_t smat_launch_state_read_dual_tc(const void* Xt, const void* Xn, const
 cudaError_t smat_launch_decode_step(const void* q, const void* k, const void* v, void* o, float* S, const void* U,
                                     int u_bf16, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
                                     cudaStream_t st, const float* log_a = nullptr, float* log_g = nullptr);
+// The same step on a packed type table (smat_decode_pack), and the packing itself: `rows` rows of p entries to int8 codes and
+// a unit each, or back (see smat_pack.cu).  `tail` bytes (a multiple of 16) behind the table are copied as they are.
+cudaError_t smat_launch_decode_step_packed(const void* q, const void* k, const void* v, void* o, float* S, const void* codes,
+                                           const float* units, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
+                                           cudaStream_t st, const float* log_a, float* log_g);
+cudaError_t smat_launch_pack(const void* table, int table_bf16, void* codes, float* units, int64_t rows, int p, const void* tail_from,
+                             void* tail_to, size_t tail, cudaStream_t st);
+cudaError_t smat_launch_unpack(const void* codes, const float* units, void* table, int table_bf16, int64_t rows, int p,
+                               const void* tail_from, void* tail_to, size_t tail, cudaStream_t st);
 // d = 3 tabulation from a bf16 profile table on the fp32 ALUs (primes too large for the resident-matrix kernel).
 int smat_tabulate_d3_bf16_slab(const SmatGeo& geo, int64_t state_elems);
 cudaError_t smat_launch_tabulate_d3_bf16(const void* in, void* out, const SmatGeo& geo, int64_t state_elems, int bh,

@@ -1,0 +1,159 @@
+// Type table of the decode cache in 8 bits, and back.  A row of p entries gets m = 127 / max|row|, cut to the eight significant bits of
+// a bf16 number: code = entry * m rounded to the nearest whole number (even between two), value = code * (1 / m).  With eight bits in m the
+// product with a bf16 entry is exact in fp32 and that with an fp32 entry in fp64, so a code is the nearest one in any
+// arithmetic; the cut costs less than 2^-7 of the range.  A code's value is off by at most half a unit, max|row| / 254 (1 + 2^-7).
+//
+// Streams: a row is held by the lanes that read it in 16-byte pieces (p = 128 of bf16: 16 lanes, 8 codes each), its largest entry
+// found by shuffles.  ROWS rows are in flight a thread.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "smat_internal.h"
+#include "smat_launch.cuh"
+#include "smat_rows.cuh"
+
+namespace {
+
+constexpr int PACK_THREADS = 256, PACK_ROWS = 4;
+
+// The CTAs behind those of the rows copy what follows the table (running states, gates).
+__device__ __forceinline__ void copy_tail(const uint4* from, uint4* to, int64_t words, int64_t block) {
+  const int64_t i = block * PACK_THREADS + threadIdx.x;
+  if (i < words) to[i] = from[i];
+}
+
+template <typename TU, int P>
+__global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const TU* table, int8_t* codes, float* units, int64_t rows,
+                                                            int64_t row_blocks, const uint4* tail_from, uint4* tail_to, int64_t tail) {
+  constexpr int VEC = 16 / (int)sizeof(TU), LANES = P / VEC, SLOTS = PACK_THREADS / LANES;
+  pdl_trigger();
+  pdl_wait();
+  if ((int64_t)blockIdx.x >= row_blocks) {
+    copy_tail(tail_from, tail_to, tail, blockIdx.x - row_blocks);
+    return;
+  }
+  const int lane = threadIdx.x % LANES;
+  const int64_t first = (int64_t)blockIdx.x * (SLOTS * PACK_ROWS) + threadIdx.x / LANES;
+  RowVec<TU, VEC> in[PACK_ROWS];
+#pragma unroll
+  for (int n = 0; n < PACK_ROWS; ++n) {
+    const int64_t row = first + n * SLOTS;
+    in[n].clear();
+    if (row < rows) in[n].load(table + row * P + lane * VEC);
+  }
+#pragma unroll
+  for (int n = 0; n < PACK_ROWS; ++n) {
+    const int64_t row = first + n * SLOTS;
+    uint32_t top = 0u;      // bits of the largest |entry|: in the order of the numbers, with inf and NaN above all of them
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) top = max(top, __float_as_uint(in[n].get(i)) & 0x7fffffffu);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const bool finite = top < 0x7f800000u;
+    float m = 0.f;
+    if (top != 0u && finite) m = __uint_as_float(__float_as_uint(fminf(__fdiv_rn(127.f, __uint_as_float(top)), 0x1p126f)) & 0xffff0000u);
+    uint32_t word[VEC / 4];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      int code;
+      if (sizeof(TU) == 2) code = __float2int_rn(in[n].get(i) * m);
+      else code = __double2int_rn((double)in[n].get(i) * (double)m);
+      if (!finite) code = 0;
+      word[i / 4] = i % 4 ? word[i / 4] | (uint32_t)(code & 0xff) << (8 * (i % 4)) : (uint32_t)(code & 0xff);
+    }
+    if (row >= rows) continue;
+    uint32_t* to = reinterpret_cast<uint32_t*>(codes + row * P + lane * VEC);
+    if constexpr (VEC == 8) *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
+    else *to = word[0];
+    if (lane == 0) units[row] = !finite ? __uint_as_float(0x7fc00000u) : m > 0.f ? __frcp_rn(m) : 0.f;
+  }
+}
+
+template <typename TU, int P>
+__global__ void __launch_bounds__(PACK_THREADS) unpack_kernel(const int8_t* codes, const float* units, TU* table, int64_t rows,
+                                                              int64_t row_blocks, const uint4* tail_from, uint4* tail_to, int64_t tail) {
+  constexpr int VEC = 16 / (int)sizeof(TU), LANES = P / VEC, SLOTS = PACK_THREADS / LANES;
+  pdl_trigger();
+  pdl_wait();
+  if ((int64_t)blockIdx.x >= row_blocks) {
+    copy_tail(tail_from, tail_to, tail, blockIdx.x - row_blocks);
+    return;
+  }
+  const int lane = threadIdx.x % LANES;
+  const int64_t first = (int64_t)blockIdx.x * (SLOTS * PACK_ROWS) + threadIdx.x / LANES;
+  RowVec<float, VEC / 4> in[PACK_ROWS];      // VEC codes
+  float unit[PACK_ROWS];
+#pragma unroll
+  for (int n = 0; n < PACK_ROWS; ++n) {
+    const int64_t row = first + n * SLOTS;
+    if (row >= rows) break;
+    in[n].load(reinterpret_cast<const float*>(codes + row * P + lane * VEC));
+    unit[n] = units[row];
+  }
+#pragma unroll
+  for (int n = 0; n < PACK_ROWS; ++n) {
+    const int64_t row = first + n * SLOTS;
+    if (row >= rows) break;
+    float v[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = (float)(int8_t)(in[n].w[i / 4] >> (8 * (i % 4))) * unit[n];
+    if (unit[n] > 0x1p120f) {      // half a unit above an entry at the end of the type's range: its largest number
+      const float most = sizeof(TU) == 2 ? 0x1.fep127f : 0x1.fffffep127f;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = fminf(fmaxf(v[i], -most), most);
+    }
+    RowVec<TU, VEC> out;
+    out.set(v);
+    out.store(table + row * P + lane * VEC);
+  }
+}
+
+struct Blocks {
+  int64_t rows, all, words;
+};
+template <typename TU, int P>
+Blocks blocks(int64_t rows, size_t tail) {
+  constexpr int PER = PACK_THREADS / (P / (16 / (int)sizeof(TU))) * PACK_ROWS;
+  Blocks b;
+  b.rows = (rows + PER - 1) / PER;
+  b.words = (int64_t)(tail / 16);
+  b.all = b.rows + (b.words + PACK_THREADS - 1) / PACK_THREADS;
+  return b;
+}
+
+template <typename TU, int P>
+cudaError_t pack(const void* table, void* codes, float* units, int64_t rows, const void* from, void* to, size_t tail, cudaStream_t st) {
+  const Blocks b = blocks<TU, P>(rows, tail);
+  if (b.all > INT32_MAX) return cudaErrorInvalidValue;
+  return smat_launch_pdl(pack_kernel<TU, P>, dim3((unsigned)b.all), PACK_THREADS, 0, st, static_cast<const TU*>(table),
+                         static_cast<int8_t*>(codes), units, rows, b.rows, static_cast<const uint4*>(from), static_cast<uint4*>(to), b.words);
+}
+template <typename TU, int P>
+cudaError_t unpack(const void* codes, const float* units, void* table, int64_t rows, const void* from, void* to, size_t tail, cudaStream_t st) {
+  const Blocks b = blocks<TU, P>(rows, tail);
+  if (b.all > INT32_MAX) return cudaErrorInvalidValue;
+  return smat_launch_pdl(unpack_kernel<TU, P>, dim3((unsigned)b.all), PACK_THREADS, 0, st, static_cast<const int8_t*>(codes), units,
+                         static_cast<TU*>(table), rows, b.rows, static_cast<const uint4*>(from), static_cast<uint4*>(to), b.words);
+}
+
+}  // namespace
+
+cudaError_t smat_launch_pack(const void* table, int table_bf16, void* codes, float* units, int64_t rows, int p, const void* tail_from,
+                             void* tail_to, size_t tail, cudaStream_t st) {
+  if ((p != 64 && p != 128) || tail % 16) return cudaErrorInvalidValue;
+  if (table_bf16)
+    return p == 64 ? pack<__nv_bfloat16, 64>(table, codes, units, rows, tail_from, tail_to, tail, st)
+                   : pack<__nv_bfloat16, 128>(table, codes, units, rows, tail_from, tail_to, tail, st);
+  return p == 64 ? pack<float, 64>(table, codes, units, rows, tail_from, tail_to, tail, st)
+                 : pack<float, 128>(table, codes, units, rows, tail_from, tail_to, tail, st);
+}
+
+cudaError_t smat_launch_unpack(const void* codes, const float* units, void* table, int table_bf16, int64_t rows, int p,
+                               const void* tail_from, void* tail_to, size_t tail, cudaStream_t st) {
+  if ((p != 64 && p != 128) || tail % 16) return cudaErrorInvalidValue;
+  if (table_bf16)
+    return p == 64 ? unpack<__nv_bfloat16, 64>(codes, units, table, rows, tail_from, tail_to, tail, st)
+                   : unpack<__nv_bfloat16, 128>(codes, units, table, rows, tail_from, tail_to, tail, st);
+  return p == 64 ? unpack<float, 64>(codes, units, table, rows, tail_from, tail_to, tail, st)
+                 : unpack<float, 128>(codes, units, table, rows, tail_from, tail_to, tail, st);
+}
