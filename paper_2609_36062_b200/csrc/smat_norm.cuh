@@ -1,0 +1,149 @@
+// What the norm's two directions share: arguments, the layout of a row over lanes, sums over a row, the gate's function.
+//
+// A row of `width` columns belongs to `lanes` lanes (a power of two), each with E columns of it in registers, VEC at a time: columns
+// (n * lanes + lane) * VEC for n < E / VEC.  Rows of a head are held by part of a warp or a warp and meet by shuffles; rows of a
+// model by a CTA.  A CTA's rows all belong to one group, so that its weights stay in registers while it walks over the rows;
+// the next row is on its way while one is summed.  Groups are the fastest part of the CTA's number: the CTAs that run together
+// cover the same tokens of all groups, whichever of the two layouts ([b, h, T, d] or [b, T, h, d]) a tensor has.
+#pragma once
+#include <cuda_runtime.h>
+
+#include "smat_launch.cuh"
+#include "smat_rows.cuh"
+
+constexpr int NORM_MAX_WIDTH = 16384;
+constexpr int NORM_SMS = 148;
+
+// An operand, and by how much a thread's element of it moves from one tile of a CTA to the next: `step`, and `wrap` more where the
+// next tile belongs to the next sequence.
+struct NormOperand {
+  void* data;
+  RowStride at;
+  int64_t step, wrap;
+};
+struct NormArgs {
+  NormOperand x, residual, gate, dy, dh_in, y, h, dh, dx, dgate;
+  const float *weight, *scale;
+  int64_t weight_group;
+  float *dw, *ds;             // partial rows [groups][CTAs of a group][width], or null
+  uint32_t batch, T;          // (1, batch * T) where every operand has its sequences one behind the other
+  uint32_t tiles;             // of a sequence: as many tokens as a CTA has rows
+  uint32_t groups, ctas;      // CTAs of a group
+  uint32_t step_batch, step_tile;   // ctas = step_batch * tiles + step_tile
+  int width, lanes;
+  float eps, inv_width;
+  int sigmoid;
+};
+
+// A CTA's place in its walk over the tiles: sequence b, tile i of it.
+struct NormWalk {
+  uint32_t b, i, slots, slot;
+  bool wrapped;
+  __device__ __forceinline__ NormWalk(const NormArgs& a)
+      : slots(blockDim.x / a.lanes), slot(threadIdx.x / a.lanes), wrapped(false) {
+    const uint32_t tile = blockIdx.x / a.groups;
+    b = tile / a.tiles;
+    i = tile - b * a.tiles;
+  }
+  __device__ __forceinline__ void next(const NormArgs& a) {
+    b += a.step_batch;
+    i += a.step_tile;
+    wrapped = i >= a.tiles;
+    if (wrapped) {
+      i -= a.tiles;
+      ++b;
+    }
+  }
+  __device__ __forceinline__ bool more(const NormArgs& a) const { return b < a.batch; }
+  __device__ __forceinline__ bool in(const NormArgs& a) const { return b < a.batch && i * slots + slot < a.T; }
+  template <typename T>
+  __device__ __forceinline__ T* seat(const NormOperand& o, uint32_t g, int col) const {
+    return static_cast<T*>(o.data) + b * o.at.batch + g * o.at.head + (i * slots + slot) * o.at.token + col;
+  }
+};
+template <typename T>
+__device__ __forceinline__ void norm_move(T*& p, const NormOperand& o, bool wrapped) {
+  p += o.step;
+  if (wrapped) p += o.wrap;
+}
+
+// What a kernel is compiled for: rows alone, with the residual stream (forward) or the branch's scale (backward), behind a block with
+// one of the gates, or anything, decided by the operands that are given (rows that move by one or two elements only have this one).
+// A kernel that asks at run time issues twice the instructions of one that does not, and it is instructions that bound the gated
+// norms of heads.
+enum NormMode { NORM_ROWS, NORM_STREAM, NORM_SILU, NORM_SIGMOID, NORM_ANY };
+
+// Pairs of columns: one instruction for both (FFMA2 and its like).
+__device__ __forceinline__ float2 norm_both(float v) { return make_float2(v, v); }
+template <int VEC, int E, typename V>
+__device__ __forceinline__ float2 norm_pair(const V (&v)[E / VEC], int j) {
+  return make_float2(v[2 * j / VEC].get(2 * j % VEC), v[(2 * j + 1) / VEC].get((2 * j + 1) % VEC));
+}
+
+template <typename T>
+__device__ __forceinline__ float2 norm_sigmoid(float2 z) {
+  if constexpr (sizeof(T) == 4) {
+    return make_float2(1.f / (1.f + expf(-z.x)), 1.f / (1.f + expf(-z.y)));
+  } else {      // rounded to bf16 soon: powers and reciprocals within 2^-22, results below 2^-126 zero
+    float2 e = __fmul2_rn(z, norm_both(-1.4426950408889634f)), r;
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e.y));
+    e = __fadd2_rn(e, norm_both(1.f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(e.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(e.y));
+    return r;
+  }
+}
+
+// Sums over the lanes of a row, the same in each of them.  `turn` alternates between the two halves of the exchange buffer, so
+// that one barrier a sum is enough.
+template <int N>
+__device__ __forceinline__ void norm_row_sum(float (&v)[N], int lanes, int turn, float (*part)[N][32]) {
+  for (int o = min(lanes, 32) / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  if (lanes <= 32) return;
+  const int warp = threadIdx.x >> 5;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) part[turn & 1][i][warp] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = 0.f;
+    for (int w = 0; w < lanes / 32; ++w) v[i] += part[turn & 1][i][w];
+  }
+}
+
+// Columns a lane holds, the CTA's threads at most and the lanes, by the width alone.  Eight columns a lane as long as a CTA holds
+// the row with them: at 128 registers a thread of the backward pass keeps its row, the next one and the sums of dw and dscale
+// there without spills (sixteen columns spilled 800 bytes), and 512 threads an SM have enough on its way.
+struct NormShape {
+  int columns, threads, lanes;
+};
+inline NormShape norm_shape(int width) {
+  int columns = 8, lanes = 1;
+  while (lanes * columns < width) {
+    if (lanes < 1024) lanes *= 2;
+    else columns *= 2;
+  }
+  return {columns, lanes <= 256 ? 256 : lanes, lanes};
+}
+
+// The walk of at most `ctas` CTAs a group over tiles of `slots` tokens.
+inline void norm_walk(NormArgs* a, uint32_t slots, uint32_t ctas) {
+  a->tiles = (a->T + slots - 1) / slots;
+  const uint32_t all = a->tiles * a->batch;
+  a->ctas = ctas < 1 ? 1 : ctas > all ? all : ctas;
+  a->step_batch = a->ctas / a->tiles;
+  a->step_tile = a->ctas % a->tiles;
+  for (NormOperand* o : {&a->x, &a->residual, &a->gate, &a->dy, &a->dh_in, &a->y, &a->h, &a->dh, &a->dx, &a->dgate}) {
+    o->step = a->step_batch * o->at.batch + (int64_t)a->step_tile * slots * o->at.token;
+    o->wrap = o->at.batch - (int64_t)a->tiles * slots * o->at.token;
+  }
+}
+
+// Launchers of the two directions.  vec: elements that the rows of all operands can be moved by (16 bytes of them, 2 bf16, or 1).
+int smat_norm_partials(int groups, int width);
+cudaError_t smat_launch_norm_forward(NormArgs& a, int bf16, int vec, cudaStream_t st);
+cudaError_t smat_launch_norm_backward(NormArgs& a, int bf16, int vec, float* dw, float* ds, cudaStream_t st);

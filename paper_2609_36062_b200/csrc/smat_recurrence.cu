@@ -15,6 +15,8 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "smat_launch.cuh"
 #include "smat_rows.cuh"
 
@@ -38,6 +40,21 @@ struct RecArgs {
 // a * state + x, a closed gate forgetting the state whatever it is.
 __device__ __forceinline__ float step(float a, float state, float x) { return a == 0.f ? x : fmaf(a, state, x); }
 
+// Whether a sum of numbers times zero has met one that is not finite.  Only then does a closed gate need looking at (0 * state is
+// no zero): the loops over tokens run without it, and once more with it where the state behind them is not finite.
+__device__ __forceinline__ bool not_finite(float zeros) { return zeros != 0.f; }
+
+// Where an operand's tokens of one tile lie: the same address for all threads of a CTA, and a thread's distance from it.  So the
+// address arithmetic of a token is left to the uniform datapath (64-bit products of token and stride in every thread were
+// a fifth of all instructions).  s counts tokens in the order of the recurrence, t = s or T - 1 - s.
+template <typename T, typename OFF>
+struct Place {
+  const T* base;      // of the last thread's tokens (backward) or the first's: the lowest address
+  int64_t token;      // elements from one s to the next
+  OFF off;
+  __device__ __forceinline__ T* at(int l) const { return const_cast<T*>(base + l * token + off); }
+};
+
 // What a thread holds of a tile: VEC channels of STEPS tokens.
 template <typename TX, typename TA, int VEC, int STEPS, bool BACK>
 struct Share {
@@ -45,48 +62,120 @@ struct Share {
   RowVec<TA, VEC> a[STEPS];
   RowVec<TX, VEC> h[BACK ? STEPS : 1];
 
-  // Tokens s .. s + STEPS - 1; those from T on are left as they are (their number is `count`).
-  __device__ __forceinline__ void load(const RecArgs& p, const TX* xp, const TA* ap, const TX* hp, int64_t s, int count) {
+  // `count` tokens, and behind them tokens that leave the state as it is.  The last of `left` tokens up to the end of the
+  // sequence is token 0 of a backward pass, which has none before it.
+  template <typename OFF>
+  __device__ __forceinline__ void load(const Place<TX, OFF>& xp, const Place<TA, OFF>& ap, const Place<TX, OFF>& hp, int count, int64_t left) {
+    if (count == STEPS && (!BACK || left > STEPS)) {
+#pragma unroll
+      for (int l = 0; l < STEPS; ++l) {
+        x[l].load(xp.at(l));
+        a[l].load(ap.at(l));
+        if (BACK) h[l].load(hp.at(l));
+      }
+      return;
+    }
 #pragma unroll
     for (int l = 0; l < STEPS; ++l) {
-      if (l >= count) break;
-      const int64_t t = BACK ? p.T - 1 - (s + l) : s + l;
-      x[l].load(xp + t * p.xs.token);
-      a[l].load(ap + t * p.as.token);
-      if (BACK && t > 0) h[l].load(hp + (t - 1) * p.hs.token);
+      x[l].clear();
+      a[l].clear();
+      if (BACK) h[l].clear();
+      if (l >= count) continue;
+      x[l].load(xp.at(l));
+      a[l].load(ap.at(l));
+      if (BACK && l + 1 < left) h[l].load(hp.at(l));
     }
   }
 };
 
-// The tokens of a share from `state` on: outputs stored, `state` becomes the one behind them.
-template <typename TX, typename TA, int VEC, int STEPS, bool BACK>
-__device__ __forceinline__ void apply(const RecArgs& p, const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC],
-                                      float (&state)[VEC], TX* op, TA* dap, const float* h0, int64_t s, int count) {
+// The map (A, H) of a share's tokens.
+template <bool CLOSED, typename TX, typename TA, int VEC, int STEPS, bool BACK>
+__device__ __forceinline__ void map_of(const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC], float (&A)[VEC],
+                                       float (&H)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) { A[i] = 1.f; H[i] = 0.f; }
 #pragma unroll
   for (int l = 0; l < STEPS; ++l) {
-    if (l >= count) break;
-    const int64_t t = BACK ? p.T - 1 - (s + l) : s + l;
-    float v[VEC];
-    if (BACK) {
-      float d[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        v[i] = in.x[l].get(i) + state[i];                                  // dx
-        state[i] = gate[l][i] == 0.f ? 0.f : gate[l][i] * v[i];            // c
-        const float before = t > 0 ? in.h[l].get(i) : h0 ? h0[i] : 0.f;
-        d[i] = gate[l][i] == 0.f ? 0.f : state[i] * before;
-      }
-      RowVec<TA, VEC> da;
-      da.set(d);
-      da.store(dap + t * p.das.token);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = state[i] = step(gate[l][i], state[i], in.x[l].get(i));
+    for (int i = 0; i < VEC; ++i) {
+      const float a = gate[l][i], x = in.x[l].get(i);
+      A[i] *= a;
+      if (CLOSED && a == 0.f) H[i] = BACK ? 0.f : x;
+      else H[i] = BACK ? a * (H[i] + x) : fmaf(a, H[i], x);
     }
-    RowVec<TX, VEC> o;
-    o.set(v);
-    o.store(op + t * p.os.token);
   }
+}
+
+// The tokens of a share from `state` on: outputs stored, `state` becomes the one behind them.  Returns zero if all of it is finite.
+// h0: of this thread's channels, or null; only token 0 of a backward pass, the last of `left`, looks at it.
+template <bool CLOSED, typename TX, typename TA, int VEC, int STEPS, bool BACK, typename OFF>
+__device__ __forceinline__ float apply(const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC], float (&state)[VEC],
+                                       const Place<TX, OFF>& op, const Place<TA, OFF>& dap, const float* h0, int count, int64_t left) {
+  float zeros = 0.f;
+  const bool last = BACK && left <= STEPS;
+#pragma unroll
+  for (int l = 0; l < STEPS; ++l) {
+    float v[VEC], d[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float a = gate[l][i], x = in.x[l].get(i);
+      if (BACK) {
+        v[i] = x + state[i];                                           // dx
+        state[i] = CLOSED && a == 0.f ? 0.f : a * v[i];                // c
+        float before = in.h[BACK ? l : 0].get(i);
+        if (last && l + 1 == left && h0) before = h0[i];
+        d[i] = CLOSED && a == 0.f ? 0.f : state[i] * before;
+        zeros = fmaf(d[i], 0.f, zeros);
+      } else {
+        v[i] = state[i] = CLOSED ? step(a, state[i], x) : fmaf(a, state[i], x);
+      }
+    }
+    if (l < count) {
+      RowVec<TX, VEC> o;
+      o.set(v);
+      o.store(op.at(l));
+      if constexpr (BACK) {
+        RowVec<TA, VEC> da;
+        da.set(d);
+        da.store(dap.at(l));
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) zeros = fmaf(state[i], 0.f, zeros);
+  return zeros;
+}
+
+template <typename TX, typename TA, int VEC, int STEPS, bool BACK, typename OFF>
+__device__ __forceinline__ void apply(const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC], float (&state)[VEC],
+                                      const Place<TX, OFF>& op, const Place<TA, OFF>& dap, const float* h0, int count, int64_t left) {
+  float entered[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) entered[i] = state[i];
+  if (!not_finite(apply<false>(in, gate, state, op, dap, h0, count, left))) return;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) state[i] = entered[i];
+  apply<true>(in, gate, state, op, dap, h0, count, left);
+}
+
+// exp of the log-gates.  From -4 up, 2^(x log2 e) with one rounding of the exponent: it is off by 2^-22 there, and the power by 2^-22
+// of itself; below, where the rounded exponent would cost more, expf.
+template <typename TX, typename TA, int VEC, int STEPS, bool BACK>
+__device__ __forceinline__ void gates_of(const Share<TX, TA, VEC, STEPS, BACK>& in, float (&gate)[STEPS][VEC]) {
+  float least = 0.f;
+#pragma unroll
+  for (int l = 0; l < STEPS; ++l)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float x = in.a[l].get(i);
+      least = fminf(least, x);
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(gate[l][i]) : "f"(x * 1.4426950408889634f));
+    }
+  if (least >= -4.f) return;
+#pragma unroll
+  for (int l = 0; l < STEPS; ++l)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) gate[l][i] = expf(in.a[l].get(i));
 }
 
 // Short sequences: a thread takes VEC channels of a sequence from the first token to the last.
@@ -98,27 +187,23 @@ __global__ void __launch_bounds__(REC_THREADS) recurrence_short_kernel(const Rec
   pdl_wait();
   if (n >= pieces) return;
   const int c = (int)n * VEC;
-  const TX* xp = static_cast<const TX*>(p.x) + b * p.xs.batch + c;
-  const TA* ap = static_cast<const TA*>(p.log_a) + b * p.as.batch + c;
-  const TX* hp = BACK ? static_cast<const TX*>(p.h) + b * p.hs.batch + c : nullptr;
-  TX* op = static_cast<TX*>(p.out) + b * p.os.batch + c;
-  TA* dap = BACK ? static_cast<TA*>(p.dlog_a) + b * p.das.batch + c : nullptr;
   const int64_t row = (int64_t)b * p.channels + c;
+  const auto place = [&](auto* data, const RowStride& at, int64_t s, int before) {
+    using P = Place<std::remove_const_t<std::remove_pointer_t<decltype(data)>>, uint64_t>;
+    return P{data + b * at.batch + (BACK ? p.T - 1 - s - before : s) * at.token + c, BACK ? -at.token : at.token, 0};
+  };
   float state[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) state[i] = p.begin ? p.begin[row + i] : 0.f;
   for (int64_t s = 0; s < p.T; s += STEPS) {
     const int count = (int)(p.T - s < STEPS ? p.T - s : STEPS);
     Share<TX, TA, VEC, STEPS, BACK> in;
-    in.load(p, xp, ap, hp, s, count);
+    in.load(place(static_cast<const TX*>(p.x), p.xs, s, 0), place(static_cast<const TA*>(p.log_a), p.as, s, 0),
+            place(static_cast<const TX*>(p.h), p.hs, s, 1), count, p.T - s);
     float gate[STEPS][VEC];
-#pragma unroll
-    for (int l = 0; l < STEPS; ++l) {
-      if (l >= count) break;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) gate[l][i] = expf(in.a[l].get(i));
-    }
-    apply<TX, TA, VEC, STEPS, BACK>(p, in, gate, state, op, dap, p.h0 ? p.h0 + row : nullptr, s, count);
+    gates_of(in, gate);
+    apply(in, gate, state, place(static_cast<const TX*>(p.out), p.os, s, 0), place(static_cast<const TA*>(p.dlog_a), p.das, s, 0),
+          p.h0 ? p.h0 + row : nullptr, count, p.T - s);
   }
   if (p.end) {
 #pragma unroll
@@ -127,10 +212,10 @@ __global__ void __launch_bounds__(REC_THREADS) recurrence_short_kernel(const Rec
 }
 
 // LANES lanes hold the channels of a token; a tile is REC_THREADS / LANES * STEPS tokens.
-template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK>
+template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK, typename OFF>
 __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArgs p) {
   constexpr int COLS = LANES * VEC, TILE = REC_THREADS / LANES * STEPS;
-  static_assert(COLS <= REC_THREADS, "a thread joins the warps' maps of one channel");
+  static_assert(COLS <= REC_THREADS && (LANES == 16 || LANES == 32), "a thread joins the warps' maps of one channel; halves of a warp");
   __shared__ float2 warp_map[REC_WARPS][COLS];                  // (A, H) of a warp's tokens
   __shared__ float entering[REC_WARPS][COLS];                   // the state that enters a warp's tokens
   __shared__ float2 tile_map[2][REC_MAX_CLUSTER][COLS];         // (A, H) of the cluster's tiles, this round's and the last one's
@@ -144,63 +229,63 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
   pdl_trigger();
   if (ranks > 1) cluster.sync();      // all of the cluster run before one writes to another's shared memory
   pdl_wait();
-  const TX* xp = static_cast<const TX*>(p.x) + b * p.xs.batch + c;
-  const TA* ap = static_cast<const TA*>(p.log_a) + b * p.as.batch + c;
-  const TX* hp = BACK ? static_cast<const TX*>(p.h) + b * p.hs.batch + c : nullptr;
-  TX* op = static_cast<TX*>(p.out) + b * p.os.batch + c;
-  TA* dap = BACK ? static_cast<TA*>(p.dlog_a) + b * p.das.batch + c : nullptr;
-  const float* h0 = p.h0 ? p.h0 + (int64_t)b * p.channels + c : nullptr;
+  const float* h0 = p.h0 && valid ? p.h0 + (int64_t)b * p.channels + c : nullptr;
   const int64_t row = (int64_t)b * p.channels + c0 + tid;       // of the channel whose maps this thread joins
   const bool joins = tid < COLS && c0 + tid < p.channels;
   float carry = joins && p.begin ? p.begin[row] : 0.f;
 
   const int64_t round = (int64_t)ranks * TILE;
-  int64_t s = (int64_t)rank * TILE + part * STEPS;
-  auto count_at = [&](int64_t at) { return !valid || at >= p.T ? 0 : (int)(p.T - at < STEPS ? p.T - at : STEPS); };
+  const int64_t begin = (int64_t)rank * TILE;
+  // an operand's place at this CTA's tile of round 0, `before` tokens before its own
+  const auto place = [&](auto* data, const RowStride& at, int before) {
+    using P = Place<std::remove_const_t<std::remove_pointer_t<decltype(data)>>, OFF>;
+    const int64_t t = BACK ? p.T - 1 - begin - before - (TILE - STEPS) : begin;
+    return P{data + b * at.batch + t * at.token + c0, BACK ? -at.token : at.token,
+             (OFF)((OFF)(BACK ? TILE - STEPS - part * STEPS : part * STEPS) * (OFF)at.token + (OFF)(column * VEC))};
+  };
+  auto xp = place(static_cast<const TX*>(p.x), p.xs, 0), hp = place(static_cast<const TX*>(p.h), p.hs, 1);
+  auto ap = place(static_cast<const TA*>(p.log_a), p.as, 0);
+  auto op = place(static_cast<const TX*>(p.out), p.os, 0);
+  auto dap = place(static_cast<const TA*>(p.dlog_a), p.das, 0);
+  const auto move = [&](auto& at) { at.base += round * at.token; };
+  const auto count_at = [&](int64_t at) { return !valid || at >= p.T ? 0 : (int)(p.T - at < STEPS ? p.T - at : STEPS); };
+  int64_t s = begin + part * STEPS;
   Share<TX, TA, VEC, STEPS, BACK> next;
-  next.load(p, xp, ap, hp, s, count_at(s));
+  next.load(xp, ap, hp, count_at(s), p.T - s);
   int turn = 0;
   for (int64_t first = 0; first < p.T; first += round, s += round, turn ^= 1) {
     const Share<TX, TA, VEC, STEPS, BACK> in = next;
     const int count = count_at(s);
-    next.load(p, xp, ap, hp, s + round, count_at(s + round));
+    move(xp);
+    move(ap);
+    if (BACK) move(hp);
+    next.load(xp, ap, hp, count_at(s + round), p.T - s - round);
     // the map of this thread's tokens
-    float gate[STEPS][VEC], A[VEC], H[VEC];
+    float gate[STEPS][VEC], A[VEC], H[VEC], zeros = 0.f;
+    gates_of(in, gate);
+    map_of<false>(in, gate, A, H);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) { A[i] = 1.f; H[i] = 0.f; }
+    for (int i = 0; i < VEC; ++i) zeros = fmaf(H[i], 0.f, zeros);
+    if (not_finite(zeros)) map_of<true>(in, gate, A, H);
+    // ... of the tokens before them in the warp (with 16 lanes a token: the other half's), and of all of the warp's
+    float before_A[VEC], before_H[VEC];
 #pragma unroll
-    for (int l = 0; l < STEPS; ++l) {
-      if (l >= count) break;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float a = expf(in.a[l].get(i)), x = in.x[l].get(i);
-        gate[l][i] = a;
-        A[i] *= a;
-        H[i] = BACK ? (a == 0.f ? 0.f : a * (H[i] + x)) : step(a, H[i], x);
-      }
-    }
-    // ... of the warp's tokens up to and with this thread's
-#pragma unroll
-    for (int o = LANES; o < 32; o *= 2) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const float before_A = __shfl_up_sync(0xffffffffu, A[i], o), before_H = __shfl_up_sync(0xffffffffu, H[i], o);
-        if (lane >= o) {
-          H[i] = step(A[i], before_H, H[i]);
-          A[i] = A[i] == 0.f ? 0.f : A[i] * before_A;
+    for (int i = 0; i < VEC; ++i) {
+      before_A[i] = 1.f;
+      before_H[i] = 0.f;
+      if (LANES == 16) {
+        const float a = __shfl_up_sync(0xffffffffu, A[i], 16), h = __shfl_up_sync(0xffffffffu, H[i], 16);
+        if (lane >= 16) {
+          before_A[i] = a;
+          before_H[i] = h;
+          H[i] = step(A[i], h, H[i]);
+          A[i] *= a;
         }
       }
     }
     if (lane >= 32 - LANES)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) warp_map[warp][column * VEC + i] = make_float2(A[i], H[i]);
-    // ... and up to this thread's, without it
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      const float a = __shfl_up_sync(0xffffffffu, A[i], LANES), h = __shfl_up_sync(0xffffffffu, H[i], LANES);
-      A[i] = lane >= LANES ? a : 1.f;
-      H[i] = lane >= LANES ? h : 0.f;
-    }
     __syncthreads();
     if (ranks > 1) {
       if (tid < COLS) {
@@ -208,7 +293,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
 #pragma unroll
         for (int w = 1; w < REC_WARPS; ++w) {
           const float2 n = warp_map[w][tid];
-          m = make_float2(n.x == 0.f ? 0.f : n.x * m.x, step(n.x, m.y, n.y));
+          m = make_float2(n.x * m.x, step(n.x, m.y, n.y));
         }
         for (int r = 0; r < ranks; ++r) *cluster.map_shared_rank(&tile_map[turn][rank][tid], r) = m;
       }
@@ -234,16 +319,19 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
     __syncthreads();
     float state[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) state[i] = step(A[i], entering[warp][column * VEC + i], H[i]);
-    apply<TX, TA, VEC, STEPS, BACK>(p, in, gate, state, op, dap, h0, s, count);
+    for (int i = 0; i < VEC; ++i) state[i] = step(before_A[i], entering[warp][column * VEC + i], before_H[i]);
+    apply(in, gate, state, op, dap, h0, count, p.T - s);
+    move(op);
+    if (BACK) move(dap);
   }
   if (p.end && rank == 0 && joins) p.end[row] = carry;
 }
 
+constexpr int64_t REC_NEAR = (int64_t)1 << 24;   // elements between two of a tile's 128 tokens, where 32 bits hold a tile
 constexpr int64_t REC_SHORT = 8;          // tokens up to which a thread takes a sequence by itself
 constexpr int64_t REC_CTAS = 148 * 2;     // as many as run at once
 
-template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK>
+template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK, typename OFF>
 cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   if (a.T <= REC_SHORT) {
     const uint32_t pieces = (uint32_t)((a.channels + VEC - 1) / VEC);
@@ -255,19 +343,19 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   // tiles in turn over the CTAs of a cluster until they fill the GPU
   unsigned ranks = 1;
   while (ranks < REC_MAX_CLUSTER && 2 * ranks <= tiles && columns * batch * ranks < REC_CTAS) ranks *= 2;
-  return smat_launch_pdl_cluster(recurrence_kernel<TX, TA, VEC, LANES, STEPS, BACK>, dim3(ranks, (unsigned)columns, (unsigned)batch),
+  return smat_launch_pdl_cluster(recurrence_kernel<TX, TA, VEC, LANES, STEPS, BACK, OFF>, dim3(ranks, (unsigned)columns, (unsigned)batch),
                                  REC_THREADS, 0, ranks, st, a);
 }
 
 template <bool BACK>
 cudaError_t dispatch(const RecArgs& a, const smat_recurrence_problem* p, bool wide, cudaStream_t st) {
+  constexpr int S = BACK ? 4 : 8;
+  using bf16 = __nv_bfloat16;
   if (p->dtype == SMAT_F32)
-    return wide ? launch<float, float, 4, 16, 4, BACK>(a, p->batch, st) : launch<float, float, 1, 32, 4, BACK>(a, p->batch, st);
+    return wide ? launch<float, float, 4, 16, 4, BACK, uint32_t>(a, p->batch, st) : launch<float, float, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
   if (p->gate_dtype == SMAT_BF16)
-    return wide ? launch<__nv_bfloat16, __nv_bfloat16, 8, 8, 4, BACK>(a, p->batch, st)
-                : launch<__nv_bfloat16, __nv_bfloat16, 1, 32, 4, BACK>(a, p->batch, st);
-  return wide ? launch<__nv_bfloat16, float, 4, 16, 4, BACK>(a, p->batch, st)
-              : launch<__nv_bfloat16, float, 1, 32, 4, BACK>(a, p->batch, st);
+    return wide ? launch<bf16, bf16, 4, 16, S, BACK, uint32_t>(a, p->batch, st) : launch<bf16, bf16, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
+  return wide ? launch<bf16, float, 4, 16, 4, BACK, uint32_t>(a, p->batch, st) : launch<bf16, float, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
 }
 
 struct Operand {
@@ -275,7 +363,7 @@ struct Operand {
   smat_dtype dtype;
   bool output;
 };
-// wide: 16-byte pieces of the widest operand everywhere.
+// wide: four channels at a time everywhere (8 bytes of bf16, 16 of fp32), and the tokens of a tile within 2^31 elements.
 template <int N>
 smat_status check(const smat_recurrence_problem* p, const Operand (&ops)[N], const float* const (&states)[3], bool* wide) {
   if (!p) return SMAT_ERR_NULL;
@@ -285,12 +373,12 @@ smat_status check(const smat_recurrence_problem* p, const Operand (&ops)[N], con
     return SMAT_ERR_DTYPE;
   if (p->batch < 1 || p->batch > 65535 || p->T < 1 || p->T > ((int64_t)1 << 40) || p->channels < 1 || p->channels > (1 << 20))
     return SMAT_ERR_SHAPE;
-  *wide = p->channels % (p->gate_dtype == SMAT_BF16 ? 8 : 4) == 0;
+  *wide = p->channels % 4 == 0;
   for (const Operand& o : ops)
     if (!rows_ok(o.rows, p->batch, 1, p->T, p->channels, o.output)) return SMAT_ERR_SHAPE;
   for (const Operand& o : ops) {
     if (rows_misaligned(o.rows, o.dtype)) return SMAT_ERR_ALIGN;
-    *wide = *wide && rows_in_16(o.rows, o.dtype, p->batch, 1, p->T);
+    *wide = *wide && rows_at_multiples(o.rows, o.dtype, p->batch, 1, p->T, 4 * dtype_bytes(o.dtype)) && o.rows->token <= REC_NEAR;
   }
   for (const float* s : states)
     if (reinterpret_cast<uintptr_t>(s) & 3) return SMAT_ERR_ALIGN;

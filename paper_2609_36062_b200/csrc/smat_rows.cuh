@@ -77,15 +77,18 @@ inline RowStride row_stride(const smat_rows* r) { return r ? RowStride{r->batch,
 
 inline int dtype_bytes(smat_dtype t) { return t == SMAT_BF16 ? 2 : 4; }
 
-// Whether every row of r begins at a multiple of 16 bytes (strides of dimensions of one entry do not matter).
-inline bool rows_in_16(const smat_rows* r, smat_dtype t, int64_t batch, int64_t heads, int64_t tokens) {
+// Whether every row of r begins at a multiple of `bytes` (strides of dimensions of one entry do not matter).
+inline bool rows_at_multiples(const smat_rows* r, smat_dtype t, int64_t batch, int64_t heads, int64_t tokens, unsigned bytes) {
   if (!r) return true;
   const int64_t e = dtype_bytes(t);
   uint64_t bits = reinterpret_cast<uintptr_t>(r->data);
   if (batch > 1) bits |= (uint64_t)(r->batch * e);
   if (heads > 1) bits |= (uint64_t)(r->head * e);
   if (tokens > 1) bits |= (uint64_t)(r->token * e);
-  return (bits & 15) == 0;
+  return (bits & (bytes - 1)) == 0;
+}
+inline bool rows_in_16(const smat_rows* r, smat_dtype t, int64_t batch, int64_t heads, int64_t tokens) {
+  return rows_at_multiples(r, t, batch, heads, tokens, 16);
 }
 
 inline bool rows_misaligned(const smat_rows* r, smat_dtype t) {
