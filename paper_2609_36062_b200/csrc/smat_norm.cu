@@ -5,6 +5,9 @@
 
 namespace {
 
+// Operands a kernel reads: the rows, the residual, the gate.
+__host__ __device__ constexpr int norm_operands(int mode) { return mode == NORM_ROWS ? 1 : mode == NORM_ANY ? 3 : 2; }
+
 template <typename T, int VEC, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
@@ -19,23 +22,49 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
   NormWalk at(a);
   pdl_trigger();
   pdl_wait();
+  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
+  constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
+  extern __shared__ uint4 rows_shared[];
+  NormRing<N, DEPTH> ring(rows_shared);
   RowVec<T, VEC> x[VPT], r[VPT], z[VPT];
   const T *xp = at.seat<T>(a.x, g, column), *rp = at.seat<T>(a.residual, g, column), *zp = at.seat<T>(a.gate, g, column);
   T *yp = at.seat<T>(a.y, g, column), *hp = at.seat<T>(a.h, g, column);
-  const auto load = [&](bool in) {
+  // asks for the rows of the walk's place, and moves on
+  const auto load = [&]() {
+    const bool in = at.in(a);
 #pragma unroll
     for (int n = 0; n < VPT; ++n) {
-      x[n].clear();
-      if (residual) r[n].clear();
-      if (gated) z[n].clear();
-      if (!in || column + n * apart >= a.width) continue;
-      x[n].load(xp + n * apart);
-      if (residual) r[n].load(rp + n * apart);
-      if (gated) z[n].load(zp + n * apart);
+      const bool mine = in && column + n * apart < a.width;
+      if constexpr (RING) {
+        ring.fetch(n, xp + n * apart, mine);
+        if (residual) ring.fetch(VPT + n, rp + n * apart, mine);
+        if (gated) ring.fetch((ANY ? 2 : 1) * VPT + n, zp + n * apart, mine);
+      } else {
+        x[n].clear();
+        if (residual) r[n].clear();
+        if (gated) z[n].clear();
+        if (!mine) continue;
+        x[n].load(xp + n * apart);
+        if (residual) r[n].load(rp + n * apart);
+        if (gated) z[n].load(zp + n * apart);
+      }
     }
+    if constexpr (RING) {
+      ring.fetched();
+      ring.next();
+    }
+    at.next(a);
+    norm_move(xp, a.x, at.wrapped);
+    if (residual) norm_move(rp, a.residual, at.wrapped);
+    if (gated) norm_move(zp, a.gate, at.wrapped);
   };
-  bool in = at.in(a);
-  load(in);
+  NormWalk to(a);      // the rows that are worked on
+  if constexpr (RING) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load();
+  } else {
+    load();
+  }
   float2 w[E / 2], s[E / 2];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -47,6 +76,15 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
   // (all slots of a CTA go through the same tiles, so that they meet at its barriers)
   for (int turn = 0;; ++turn) {
     float2 h[E / 2], y[E / 2], squares = norm_both(0.f);
+    if constexpr (RING) {
+      ring.wait();
+#pragma unroll
+      for (int n = 0; n < VPT; ++n) {
+        ring.read(n, x[n]);
+        if (residual) ring.read(VPT + n, r[n]);
+        if (gated) ring.read((ANY ? 2 : 1) * VPT + n, z[n]);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < E / 2; ++j) {
       h[j] = norm_pair<VEC, E>(x, j);
@@ -60,18 +98,14 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
         if (!sigmoid) y[j] = __fmul2_rn(y[j], q);
       }
     }
-    at.next(a);
-    norm_move(xp, a.x, at.wrapped);
-    if (residual) norm_move(rp, a.residual, at.wrapped);
-    if (gated) norm_move(zp, a.gate, at.wrapped);
-    const bool next_in = at.in(a);
-    load(next_in);
+    const bool here = to.in(a);
+    load();
     float sum[1] = {squares.x + squares.y};
     norm_row_sum(sum, a.lanes, turn, exchange);
     const float2 rs = norm_both(rsqrtf(fmaf(sum[0], a.inv_width, a.eps)));
 #pragma unroll
     for (int n = 0; n < VPT; ++n) {
-      if (!in || column + n * apart >= a.width) continue;
+      if (!here || column + n * apart >= a.width) continue;
       float v[VEC];
       RowVec<T, VEC> out;
       if (keeps) {
@@ -88,11 +122,12 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
       out.set(v);
       out.store(yp + n * apart);
     }
-    if (!at.more(a)) break;
-    norm_move(yp, a.y, at.wrapped);
-    if (keeps) norm_move(hp, a.h, at.wrapped);
-    in = next_in;
+    to.next(a);
+    if (!to.more(a)) break;
+    norm_move(yp, a.y, to.wrapped);
+    if (keeps) norm_move(hp, a.h, to.wrapped);
   }
+  if constexpr (RING) ring.landed();
 }
 
 template <typename T, int VEC, int E, int THREADS, int MODE>
@@ -101,7 +136,8 @@ cudaError_t launch(NormArgs& a, const NormShape& s, cudaStream_t st) {
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   // as many CTAs as run at once, a group's share of them each, but none without a row
   norm_walk(&a, slots, (uint32_t)NORM_SMS * (threads > 512 ? 1 : 768 / threads) / a.groups);
-  return smat_launch_pdl(norm_forward_kernel<T, VEC, E, THREADS, MODE>, dim3(a.ctas * a.groups), threads, 0, st, a);
+  return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, THREADS,
+                     dim3(a.ctas * a.groups), threads, st, a);
 }
 
 template <typename T, int VEC, int MODE>

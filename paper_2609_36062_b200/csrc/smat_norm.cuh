@@ -95,6 +95,37 @@ __device__ __forceinline__ float2 norm_sigmoid(float2 z) {
   }
 }
 
+// Rows on their way, for operands that move in 16-byte pieces: DEPTH rows of N operands, each thread's pieces in places of its own of
+// shared memory, filled by asynchronous copies.  Nobody else reads them, so that no barrier is needed; with the next row in
+// registers instead (24 KB an SM on the way) the gated norms of heads took 157 us for 122 us of bytes.
+template <int N, int DEPTH>
+struct NormRing {
+  uint32_t base, stride, slot = 0;
+  __device__ __forceinline__ NormRing(void* shared)
+      : base((uint32_t)__cvta_generic_to_shared(shared) + threadIdx.x * 16u), stride(blockDim.x * 16u) {}
+  __device__ __forceinline__ void fetch(int k, const void* from, bool in) const {      // zeros where it is not in
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(base + (slot * N + k) * stride), "l"(from), "r"(in ? 16 : 0)
+                 : "memory");
+  }
+  __device__ __forceinline__ void fetched() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory"); }
+  __device__ __forceinline__ void landed() const { asm volatile("cp.async.wait_all;" ::: "memory"); }
+  template <typename V>
+  __device__ __forceinline__ void read(int k, V& v) const {
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(base + (slot * N + k) * stride) : "memory");
+  }
+  __device__ __forceinline__ void next() { slot = slot + 1 == DEPTH ? 0 : slot + 1; }
+};
+// Whether a row of `operands` pieces a thread has room in shared memory (fp32 rows of more than 8192 columns do not).
+__host__ __device__ constexpr bool norm_rings(int operands, int threads) { return operands * threads * 16 <= 160 * 1024; }
+// Rows on their way for a thread: 8 pieces of 16 bytes of two operands (the forward pass of small calls: no more than every
+// kernel may take, asking for more costs a call of the runtime), 16 of more.
+__host__ __device__ constexpr int norm_depth(int operands, int threads) {
+  const int depth = (threads > 512 ? 8 : operands == 2 ? 8 : 16) / operands;
+  return depth > 5 ? 5 : depth < 1 ? 1 : depth;
+}
+
 // Sums over the lanes of a row, the same in each of them.  `turn` alternates between the two halves of the exchange buffer, so
 // that one barrier a sum is enough.
 template <int N>
@@ -141,6 +172,17 @@ inline void norm_walk(NormArgs* a, uint32_t slots, uint32_t ctas) {
     o->step = a->step_batch * o->at.batch + (int64_t)a->step_tile * slots * o->at.token;
     o->wrap = o->at.batch - (int64_t)a->tiles * slots * o->at.token;
   }
+}
+
+// A launch with a ring of `operands` pieces a row (none: 0) for each of its threads.
+template <typename Kernel>
+cudaError_t norm_launch(Kernel kernel, int operands, int most_threads, dim3 grid, uint32_t threads, cudaStream_t st, const NormArgs& a) {
+  const size_t bytes = operands && norm_rings(operands, most_threads) ? (size_t)norm_depth(operands, most_threads) * operands * threads * 16 : 0;
+  if (bytes > 36 * 1024) {      // (with what a kernel has besides, more than every kernel may take)
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (err != cudaSuccess) return err;
+  }
+  return smat_launch_pdl(kernel, grid, threads, bytes, st, a);
 }
 
 // Launchers of the two directions.  vec: elements that the rows of all operands can be moved by (16 bytes of them, 2 bf16, or 1).

@@ -8,6 +8,9 @@
 
 namespace {
 
+// Operands a kernel reads: dy, h, dh_in, and the branch's rows or the gate or both.
+__host__ __device__ constexpr int norm_operands(int mode) { return mode == NORM_ROWS ? 3 : mode == NORM_ANY ? 5 : 4; }
+
 template <typename T, int VEC, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
@@ -22,30 +25,61 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
   const uint32_t slots = at.slots, slot = at.slot;
   pdl_trigger();
   pdl_wait();
+  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
+  constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
+  constexpr int X = 3 * VPT, Z = (ANY ? 4 : 3) * VPT;      // places of the branch's rows and of the gate
+  extern __shared__ uint4 rows_shared[];
+  NormRing<N, DEPTH> ring(rows_shared);
   struct Row {
     RowVec<T, VEC> dy[VPT], h[VPT], z[GATE ? VPT : 1], x[SCALE ? VPT : 1], in[VPT];
   } next;
   const T *dyp = at.seat<T>(a.dy, g, column), *hp = at.seat<T>(a.h, g, column), *zp = at.seat<T>(a.gate, g, column);
   const T *xp = at.seat<T>(a.x, g, column), *ip = at.seat<T>(a.dh_in, g, column);
   T *dhp = at.seat<T>(a.dh, g, column), *dxp = at.seat<T>(a.dx, g, column), *dgp = at.seat<T>(a.dgate, g, column);
-  const auto load = [&](bool in) {
+  // asks for the rows of the walk's place, and moves on
+  const auto load = [&]() {
+    const bool in = at.in(a);
 #pragma unroll
     for (int n = 0; n < VPT; ++n) {
-      next.dy[n].clear();
-      next.h[n].clear();
-      if constexpr (GATE) next.z[n].clear();
-      if constexpr (SCALE) next.x[n].clear();
-      next.in[n].clear();
-      if (!in || column + n * apart >= a.width) continue;
-      next.dy[n].load(dyp + n * apart);
-      next.h[n].load(hp + n * apart);
-      if constexpr (GATE) if (gated) next.z[n].load(zp + n * apart);
-      if constexpr (SCALE) if (scaled) next.x[n].load(xp + n * apart);
-      if (more) next.in[n].load(ip + n * apart);
+      const bool mine = in && column + n * apart < a.width;
+      if constexpr (RING) {
+        ring.fetch(n, dyp + n * apart, mine);
+        ring.fetch(VPT + n, hp + n * apart, mine);
+        if (more) ring.fetch(2 * VPT + n, ip + n * apart, mine);
+        if constexpr (SCALE) if (scaled) ring.fetch(X + n, xp + n * apart, mine);
+        if constexpr (GATE) if (gated) ring.fetch(Z + n, zp + n * apart, mine);
+      } else {
+        next.dy[n].clear();
+        next.h[n].clear();
+        if constexpr (GATE) next.z[n].clear();
+        if constexpr (SCALE) next.x[n].clear();
+        next.in[n].clear();
+        if (!mine) continue;
+        next.dy[n].load(dyp + n * apart);
+        next.h[n].load(hp + n * apart);
+        if constexpr (GATE) if (gated) next.z[n].load(zp + n * apart);
+        if constexpr (SCALE) if (scaled) next.x[n].load(xp + n * apart);
+        if (more) next.in[n].load(ip + n * apart);
+      }
     }
+    if constexpr (RING) {
+      ring.fetched();
+      ring.next();
+    }
+    at.next(a);
+    norm_move(dyp, a.dy, at.wrapped);
+    norm_move(hp, a.h, at.wrapped);
+    if (gated) norm_move(zp, a.gate, at.wrapped);
+    if (scaled) norm_move(xp, a.x, at.wrapped);
+    if (more) norm_move(ip, a.dh_in, at.wrapped);
   };
-  bool next_in = at.in(a);
-  load(next_in);
+  NormWalk to(a);      // the rows that are worked on
+  if constexpr (RING) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load();
+  } else {
+    load();
+  }
   float2 w[E / 2], dw[E / 2], ds[SCALE ? E / 2 : 1];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -57,16 +91,22 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if constexpr (SCALE) ds[e / 2] = norm_both(0.f);
   }
   for (int turn = 0;; ++turn) {
-    const Row in = next;
-    const bool here = next_in;
-    at.next(a);
-    norm_move(dyp, a.dy, at.wrapped);
-    norm_move(hp, a.h, at.wrapped);
-    if (gated) norm_move(zp, a.gate, at.wrapped);
-    if (scaled) norm_move(xp, a.x, at.wrapped);
-    if (more) norm_move(ip, a.dh_in, at.wrapped);
-    next_in = at.in(a);
-    load(next_in);
+    Row in;
+    const bool here = to.in(a);
+    if constexpr (RING) {
+      ring.wait();
+#pragma unroll
+      for (int n = 0; n < VPT; ++n) {
+        ring.read(n, in.dy[n]);
+        ring.read(VPT + n, in.h[n]);
+        if (more) ring.read(2 * VPT + n, in.in[n]);
+        if constexpr (SCALE) if (scaled) ring.read(X + n, in.x[n]);
+        if constexpr (GATE) if (gated) ring.read(Z + n, in.z[n]);
+      }
+    } else {
+      in = next;
+      load();
+    }
     // u = dy act, and what dgate is but for n: dy w act'
     float2 u[E / 2], slope[GATE ? E / 2 : 1], squares = norm_both(0.f), products = norm_both(0.f);
 #pragma unroll
@@ -84,6 +124,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
       squares = __ffma2_rn(v, v, squares);
       products = __ffma2_rn(__fmul2_rn(u[j], w[j]), v, products);
     }
+    if constexpr (RING) load();      // (into the places that have just been read)
     float sum[2] = {squares.x + squares.y, products.x + products.y};
     norm_row_sum(sum, a.lanes, turn, exchange);
     const float r = rsqrtf(fmaf(sum[0], a.inv_width, a.eps));
@@ -96,7 +137,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
       dw[j] = __ffma2_rn(u[j], n, dw[j]);
       dh[j] = __ffma2_rn(__fmul2_rn(u[j], w[j]), rs, __fmul2_rn(n, mean));
       if (more) dh[j] = __fadd2_rn(dh[j], norm_pair<VEC, E>(in.in, j));
-      if constexpr (SCALE) ds[j] = __ffma2_rn(norm_pair<VEC, E>(in.x, j), dh[j], ds[j]);
+      if constexpr (SCALE) if (scaled) ds[j] = __ffma2_rn(norm_pair<VEC, E>(in.x, j), dh[j], ds[j]);
     }
 #pragma unroll
     for (int n = 0; n < VPT; ++n) {
@@ -126,11 +167,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
         }
       }
     }
-    if (!at.more(a)) break;
-    norm_move(dhp, a.dh, at.wrapped);
-    if (branch) norm_move(dxp, a.dx, at.wrapped);
-    if (gated) norm_move(dgp, a.dgate, at.wrapped);
+    to.next(a);
+    if (!to.more(a)) break;
+    norm_move(dhp, a.dh, to.wrapped);
+    if (branch) norm_move(dxp, a.dx, to.wrapped);
+    if (gated) norm_move(dgp, a.dgate, to.wrapped);
   }
+  if constexpr (RING) ring.landed();
   // this CTA's partial rows: the slots of a column in order
   __shared__ float sums[THREADS == 256 ? 256 * E : 1];
 #pragma unroll
@@ -205,7 +248,8 @@ cudaError_t launch(NormArgs& a, const NormShape& s, float* dw, float* ds, cudaSt
   a.lanes = s.lanes;
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   norm_walk(&a, slots, (uint32_t)smat_norm_partials((int)a.groups, a.width) / a.groups);
-  cudaError_t err = smat_launch_pdl(norm_backward_kernel<T, VEC, E, THREADS, MODE>, dim3(a.ctas * a.groups), threads, 0, st, a);
+  cudaError_t err = norm_launch(norm_backward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0,
+                                THREADS, dim3(a.ctas * a.groups), threads, st, a);
   if (err != cudaSuccess || (!dw && !ds)) return err;
   const int grouped = a.weight_group ? 1 : 0;
   const dim3 grid((unsigned)((a.width + SUM_COLS - 1) / SUM_COLS), ds ? 2u : 1u, grouped ? a.groups : 1u);
