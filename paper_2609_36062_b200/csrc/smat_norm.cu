@@ -12,7 +12,7 @@ template <typename T, int VEC, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
   constexpr bool ANY = MODE == NORM_ANY;
-  __shared__ float exchange[2][1][32];
+  __shared__ float exchange[2][32][1];
   const bool residual = MODE == NORM_STREAM || (ANY && a.residual.data), keeps = (ANY || MODE == NORM_STREAM) && a.h.data;
   const bool scaled = MODE == NORM_STREAM || ANY;
   const bool gated = MODE == NORM_SILU || MODE == NORM_SIGMOID || (ANY && a.gate.data);

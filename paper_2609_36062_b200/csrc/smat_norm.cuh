@@ -126,24 +126,24 @@ __host__ __device__ constexpr int norm_depth(int operands, int threads) {
   return depth > 5 ? 5 : depth < 1 ? 1 : depth;
 }
 
-// Sums over the lanes of a row, the same in each of them.  `turn` alternates between the two halves of the exchange buffer, so
-// that one barrier a sum is enough.
+// Sums over the lanes of a row, the same in each of them: inside a warp by shuffles, then one word of shared memory a warp and
+// shuffles again.  `turn` alternates between the two halves of the exchange buffer, so that one barrier a sum is enough.
 template <int N>
-__device__ __forceinline__ void norm_row_sum(float (&v)[N], int lanes, int turn, float (*part)[N][32]) {
+__device__ __forceinline__ void norm_row_sum(float (&v)[N], int lanes, int turn, float (*part)[32][N]) {
   for (int o = min(lanes, 32) / 2; o > 0; o >>= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   if (lanes <= 32) return;
-  const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0)
+  const int warps = lanes / 32, lane = threadIdx.x & 31;
+  if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) part[turn & 1][i][warp] = v[i];
+    for (int i = 0; i < N; ++i) part[turn & 1][threadIdx.x >> 5][i] = v[i];
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = 0.f;
-    for (int w = 0; w < lanes / 32; ++w) v[i] += part[turn & 1][i][w];
-  }
+  for (int i = 0; i < N; ++i) v[i] = part[turn & 1][lane & (warps - 1)][i];
+  for (int o = warps / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
 // Columns a lane holds, the CTA's threads at most and the lanes, by the width alone.  Eight columns a lane as long as a CTA holds

@@ -15,7 +15,7 @@ template <typename T, int VEC, int E, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
   constexpr bool ANY = MODE == NORM_ANY, SCALE = ANY || MODE == NORM_STREAM, GATE = ANY || MODE == NORM_SILU || MODE == NORM_SIGMOID;
-  __shared__ float exchange[2][2][32];
+  __shared__ __align__(8) float exchange[2][32][2];
   const bool scaled = MODE == NORM_STREAM || (ANY && a.ds), branch = SCALE && a.dx.data, more = a.dh_in.data != nullptr;
   const bool gated = MODE == NORM_SILU || MODE == NORM_SIGMOID || (ANY && a.gate.data);
   const bool sigmoid = MODE == NORM_SIGMOID || (ANY && a.sigmoid);
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
   } else {
     load();
   }
-  float2 w[E / 2], dw[E / 2], ds[SCALE ? E / 2 : 1];
+  float2 w[E / 2], dw[E / 2], ds[SCALE ? E / 2 : 1], factor[SCALE ? E / 2 : 1];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int col = column + e / VEC * apart + e % VEC;
@@ -88,7 +88,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if (e % 2) w[e / 2].y = v;
     else w[e / 2].x = v;
     dw[e / 2] = norm_both(0.f);
-    if constexpr (SCALE) ds[e / 2] = norm_both(0.f);
+    if constexpr (SCALE) {
+      ds[e / 2] = norm_both(0.f);
+      const float f = branch && col < a.width ? a.scale[col] : 0.f;
+      if (e % 2) factor[e / 2].y = f;
+      else factor[e / 2].x = f;
+    }
   }
   for (int turn = 0;; ++turn) {
     Row in;
@@ -141,8 +146,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     }
 #pragma unroll
     for (int n = 0; n < VPT; ++n) {
-      const int col = column + n * apart;
-      if (!here || col >= a.width) continue;
+      if (!here || column + n * apart >= a.width) continue;
       const auto at_pair = [&](const float2* v, int i) { return (n * VEC + i) % 2 ? v[(n * VEC + i) / 2].y : v[(n * VEC + i) / 2].x; };
       float v[VEC];
       RowVec<T, VEC> out;
@@ -161,7 +165,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
       if constexpr (SCALE) {
         if (branch) {
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) v[i] = at_pair(dh, i) * a.scale[col + i];
+          for (int i = 0; i < VEC; ++i) v[i] = at_pair(dh, i) * at_pair(factor, i);
           out.set(v);
           out.store(dxp + n * apart);
         }

@@ -12,37 +12,13 @@
 // round, no flags in global memory, and sums in an order that is the same from run to run.
 //
 // Bound by HBM.  A closed gate (a = 0) drops what came before it, also where that is not finite.
-#include <cooperative_groups.h>
-#include <cuda_runtime.h>
-
 #include <type_traits>
 
-#include "smat_launch.cuh"
-#include "smat_rows.cuh"
+#include "smat_recurrence.cuh"
 
 namespace {
 
 namespace cg = cooperative_groups;
-
-constexpr int REC_THREADS = 256, REC_WARPS = REC_THREADS / 32, REC_MAX_CLUSTER = 8;
-
-struct RecArgs {
-  const void *x, *log_a, *h;      // forward: x; backward: dh and the h that was kept
-  void *out, *dlog_a;             // forward: h; backward: dx
-  RowStride xs, as, hs, os, das;
-  const float *begin;             // the state that enters the first token in the order of the recurrence (h0, dhT), or null
-  const float *h0;                // backward: the state before token 0, or null
-  float* end;                     // the state behind the last (hT, dh0), or null
-  int64_t T;
-  int channels;
-};
-
-// a * state + x, a closed gate forgetting the state whatever it is.
-__device__ __forceinline__ float step(float a, float state, float x) { return a == 0.f ? x : fmaf(a, state, x); }
-
-// Whether a sum of numbers times zero has met one that is not finite.  Only then does a closed gate need looking at (0 * state is
-// no zero): the loops over tokens run without it, and once more with it where the state behind them is not finite.
-__device__ __forceinline__ bool not_finite(float zeros) { return zeros != 0.f; }
 
 // Where an operand's tokens of one tile lie: the same address for all threads of a CTA, and a thread's distance from it.  So the
 // address arithmetic of a token is left to the uniform datapath (64-bit products of token and stride in every thread were
@@ -127,7 +103,7 @@ __device__ __forceinline__ float apply(const Share<TX, TA, VEC, STEPS, BACK>& in
         d[i] = CLOSED && a == 0.f ? 0.f : state[i] * before;
         zeros = fmaf(d[i], 0.f, zeros);
       } else {
-        v[i] = state[i] = CLOSED ? step(a, state[i], x) : fmaf(a, state[i], x);
+        v[i] = state[i] = CLOSED ? rec_step(a, state[i], x) : fmaf(a, state[i], x);
       }
     }
     if (l < count) {
@@ -152,7 +128,7 @@ __device__ __forceinline__ void apply(const Share<TX, TA, VEC, STEPS, BACK>& in,
   float entered[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) entered[i] = state[i];
-  if (!not_finite(apply<false>(in, gate, state, op, dap, h0, count, left))) return;
+  if (!rec_not_finite(apply<false>(in, gate, state, op, dap, h0, count, left))) return;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) state[i] = entered[i];
   apply<true>(in, gate, state, op, dap, h0, count, left);
@@ -266,7 +242,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
     map_of<false>(in, gate, A, H);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) zeros = fmaf(H[i], 0.f, zeros);
-    if (not_finite(zeros)) map_of<true>(in, gate, A, H);
+    if (rec_not_finite(zeros)) map_of<true>(in, gate, A, H);
     // ... of the tokens before them in the warp (with 16 lanes a token: the other half's), and of all of the warp's
     float before_A[VEC], before_H[VEC];
 #pragma unroll
@@ -278,7 +254,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
         if (lane >= 16) {
           before_A[i] = a;
           before_H[i] = h;
-          H[i] = step(A[i], h, H[i]);
+          H[i] = rec_step(A[i], h, H[i]);
           A[i] *= a;
         }
       }
@@ -293,7 +269,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
 #pragma unroll
         for (int w = 1; w < REC_WARPS; ++w) {
           const float2 n = warp_map[w][tid];
-          m = make_float2(n.x * m.x, step(n.x, m.y, n.y));
+          m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
         }
         for (int r = 0; r < ranks; ++r) *cluster.map_shared_rank(&tile_map[turn][rank][tid], r) = m;
       }
@@ -305,21 +281,21 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
         for (int r = 0; r < ranks; ++r) {
           if (r == rank) state = behind;
           const float2 m = tile_map[turn][r][tid];
-          behind = step(m.x, behind, m.y);
+          behind = rec_step(m.x, behind, m.y);
         }
       }
 #pragma unroll
       for (int w = 0; w < REC_WARPS; ++w) {
         entering[w][tid] = state;
         const float2 m = warp_map[w][tid];
-        state = step(m.x, state, m.y);
+        state = rec_step(m.x, state, m.y);
       }
       carry = ranks > 1 ? behind : state;
     }
     __syncthreads();
     float state[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) state[i] = step(before_A[i], entering[warp][column * VEC + i], before_H[i]);
+    for (int i = 0; i < VEC; ++i) state[i] = rec_step(before_A[i], entering[warp][column * VEC + i], before_H[i]);
     apply(in, gate, state, op, dap, h0, count, p.T - s);
     move(op);
     if (BACK) move(dap);
@@ -329,7 +305,6 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
 
 constexpr int64_t REC_NEAR = (int64_t)1 << 24;   // elements between two of a tile's 128 tokens, where 32 bits hold a tile
 constexpr int64_t REC_SHORT = 8;          // tokens up to which a thread takes a sequence by itself
-constexpr int64_t REC_CTAS = 148 * 2;     // as many as run at once
 
 template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK, typename OFF>
 cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
@@ -340,15 +315,16 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   }
   constexpr int COLS = LANES * VEC, TILE = REC_THREADS / LANES * STEPS;
   const int64_t columns = (a.channels + COLS - 1) / COLS, tiles = (a.T + TILE - 1) / TILE;
-  // tiles in turn over the CTAs of a cluster until they fill the GPU
-  unsigned ranks = 1;
-  while (ranks < REC_MAX_CLUSTER && 2 * ranks <= tiles && columns * batch * ranks < REC_CTAS) ranks *= 2;
+  const unsigned ranks = rec_ranks(columns, batch, tiles);
   return smat_launch_pdl_cluster(recurrence_kernel<TX, TA, VEC, LANES, STEPS, BACK, OFF>, dim3(ranks, (unsigned)columns, (unsigned)batch),
                                  REC_THREADS, 0, ranks, st, a);
 }
 
 template <bool BACK>
 cudaError_t dispatch(const RecArgs& a, const smat_recurrence_problem* p, bool wide, cudaStream_t st) {
+  const int x_bf16 = p->dtype == SMAT_BF16, gate_bf16 = p->gate_dtype == SMAT_BF16;
+  if (a.T > REC_SHORT && smat_recurrence_tma_supported(a, p->batch, x_bf16, gate_bf16, BACK))
+    return smat_launch_recurrence_tma(a, p->batch, x_bf16, gate_bf16, BACK, st);
   constexpr int S = BACK ? 4 : 8;
   using bf16 = __nv_bfloat16;
   if (p->dtype == SMAT_F32)

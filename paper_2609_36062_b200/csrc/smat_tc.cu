@@ -1877,6 +1877,21 @@ bool smat_make_map_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner, u
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Rows of features, [batch][rows][inner] with any strides in bytes (multiples of 16), fp32 or bf16; box = box_inner x box_rows of one
+// sequence, not swizzled.
+bool smat_make_map_rows(CUtensorMap* map, const void* base, int bytes, uint64_t inner, uint64_t rows, uint64_t batch, uint64_t row_stride,
+                        uint64_t batch_stride, uint32_t box_inner, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)row_stride, (cuuint64_t)batch_stride};
+  const cuuint32_t box[3] = {box_inner, box_rows, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(base), dims, strides,
+            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // The library holds sm_100a code only: the current device must be compute capability 10.x, and the driver must
 // export the tensor-map encoder the TMA kernels need.
 bool smat_tc_available() {

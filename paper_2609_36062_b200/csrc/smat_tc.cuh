@@ -9,6 +9,10 @@
 bool smat_make_map_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint32_t box_inner,
                            uint32_t box_rows, int swizzle128);
 
+// The same for rows of features at any strides (see smat_tc.cu).
+bool smat_make_map_rows(CUtensorMap* map, const void* base, int bytes, uint64_t inner, uint64_t rows, uint64_t batch, uint64_t row_stride,
+                        uint64_t batch_stride, uint32_t box_inner, uint32_t box_rows);
+
 namespace tc {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
