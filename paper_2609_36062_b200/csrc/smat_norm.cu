@@ -20,7 +20,6 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
   const uint32_t g = blockIdx.x % a.groups;
   const int lane = threadIdx.x % a.lanes, column = lane * VEC, apart = a.lanes * VEC;
   NormWalk at(a);
-  pdl_trigger();
   pdl_wait();
   constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
   constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
@@ -127,6 +126,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
     norm_move(yp, a.y, to.wrapped);
     if (keeps) norm_move(hp, a.h, to.wrapped);
   }
+  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
   if constexpr (RING) ring.landed();
 }
 

@@ -23,7 +23,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
   const int lane = threadIdx.x % a.lanes, column = lane * VEC, apart = a.lanes * VEC;
   NormWalk at(a);
   const uint32_t slots = at.slots, slot = at.slot;
-  pdl_trigger();
   pdl_wait();
   constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
   constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
@@ -177,6 +176,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if (branch) norm_move(dxp, a.dx, to.wrapped);
     if (gated) norm_move(dgp, a.dgate, to.wrapped);
   }
+  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
   if constexpr (RING) ring.landed();
   // this CTA's partial rows: the slots of a column in order
   __shared__ float sums[THREADS == 256 ? 256 * E : 1];

@@ -202,7 +202,6 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
   const uint32_t b = blockIdx.z;
   const int c0 = blockIdx.y * COLS, c = c0 + column * VEC;
   const bool valid = c < p.channels;
-  pdl_trigger();
   if (ranks > 1) cluster.sync();      // all of the cluster run before one writes to another's shared memory
   pdl_wait();
   const float* h0 = p.h0 && valid ? p.h0 + (int64_t)b * p.channels + c : nullptr;
@@ -300,6 +299,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
     move(op);
     if (BACK) move(dap);
   }
+  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
   if (p.end && rank == 0 && joins) p.end[row] = carry;
 }
 

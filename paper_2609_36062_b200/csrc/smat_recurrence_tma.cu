@@ -1,31 +1,34 @@
 // The recurrence of long sequences whose tiles move by TMA (see smat_recurrence.cu for how tiles, warps and threads are joined).
 //
-// A tile is 64 channels of 16 * STEPS tokens of every operand, in one stage of a ring in shared memory; outputs take the place of
-// the inputs there and leave by TMA too.  A thread has four channels of STEPS tokens: it forms their map, and goes over
-// them again from the state that enters them.  So loads and stores cost a thread one instruction of a fixed offset a token,
-// where their addresses had taken a third of all it issued, and the next tiles are on their way without registers.  Tokens behind
-// the end, and channels beyond the last, are read as zeros: x = 0 and log_a = 0 leave the state as it is.  A backward pass goes
-// over the same tiles from the last to the first, and reads h one token before dh.
+// A tile is 64 channels of 8 * STEPS tokens of every operand, in one stage of a ring in shared memory; outputs take the place of
+// the inputs there and leave by TMA too.  A warp has STEPS tokens of it, a thread two channels of these: it forms their map, and
+// goes over them again from the state that enters them.  So loads and stores cost a thread one instruction of a fixed offset a
+// token, where their addresses had taken a third of all it issued, and the next tiles are on their way without registers.
+// Tokens behind the end, and channels beyond the last, are read as zeros: x = 0 and log_a = 0 leave the state as it is.  A
+// backward pass goes over the same tiles from the last to the first, and reads h one token before dh.
 //
 // The CTAs of a cluster exchange the maps of their tiles by stores into one another's shared memory that complete on the reader's
-// mbarrier.  (A cluster barrier a round, which waits for all of a CTA's writes, was the longest stall.)  A rank that sends the map
-// of round n + 1 has read those of round n, so two buffers are enough.
-#include "smat_recurrence.cuh"
+// mbarrier (a cluster barrier a round, which waits for all of a CTA's writes, was the longest stall).  They are formed a round
+// ahead, so that a round hides their way.  What sends the map of round n + 1 comes after a barrier behind all reads of those of
+// round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
+//
+// It is the number of instructions that bounds it: 64 K tokens of 2048 bf16 channels took MEASURED
 #include <type_traits>
 
+#include "smat_recurrence.cuh"
 #include "smat_tc.cuh"
 
 namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int COLS = 64, VEC = 4, LANES = COLS / VEC, PARTS = REC_THREADS / LANES;
-constexpr int PORTER = REC_THREADS - 32;      // the thread that issues copies: not of the warps that join maps
+constexpr int COLS = 64, VEC = 2;
+constexpr int PORTER = REC_THREADS - 32;      // the thread that issues copies
 constexpr long long WAIT_LIMIT = 4000000000LL;   // SM clock cycles before a wait gives up
 
 template <typename TX, typename TA, int STEPS, bool BACK>
 struct Tile {
-  static constexpr int TOKENS = PARTS * STEPS;
+  static constexpr int TOKENS = REC_WARPS * STEPS;
   static constexpr uint32_t X = TOKENS * COLS * sizeof(TX), A = TOKENS * COLS * sizeof(TA);
   static constexpr uint32_t BYTES = X + A + (BACK ? X : 0);
   static constexpr uint32_t A_AT = X, H_AT = X + A;
@@ -53,13 +56,15 @@ __device__ __forceinline__ void wait_sent(uint64_t* bar, uint32_t parity, bool& 
   while (!lost && !try_wait_sent(bar, parity)) lost = clock64() - start > WAIT_LIMIT;
 }
 
-__device__ __forceinline__ void send(void* to, int rank, uint64_t* bar, float2 v) {
-  asm volatile(
-      "{\n.reg .b32 a, b;\n"
-      "mapa.shared::cluster.u32 a, %0, %2;\n"
-      "mapa.shared::cluster.u32 b, %1, %2;\n"
-      "st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [a], {%3, %4}, [b];\n}\n"
-      ::"r"(tc::smem_u32(to)), "r"(tc::smem_u32(bar)), "r"(rank), "f"(v.x), "f"(v.y) : "memory");
+// An address of this CTA's shared memory in that of another of the cluster.
+__device__ __forceinline__ uint32_t in_rank(const void* p, int rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(tc::smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void send(uint32_t to, uint32_t bar, float2 v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%2, %3}, [%1];" ::"r"(to), "r"(bar), "f"(v.x), "f"(v.y)
+               : "memory");
 }
 
 __device__ __forceinline__ void store_tile(const CUtensorMap* map, const void* from, int x, int y, int z) {
@@ -67,29 +72,60 @@ __device__ __forceinline__ void store_tile(const CUtensorMap* map, const void* f
                ::"l"(map), "r"(tc::smem_u32(from)), "r"(x), "r"(y), "r"(z) : "memory");
 }
 
+// Two channels of a token in shared memory.
 template <typename T>
-__device__ __forceinline__ void load_piece(RowVec<T, VEC>& v, const char* p) {
+__device__ __forceinline__ RowVec<T, VEC> load_piece(const char* p) {
+  RowVec<T, VEC> v;
   if constexpr (sizeof(T) == 2) {
+    v.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
     const uint2 w = *reinterpret_cast<const uint2*>(p);
     v.w[0] = w.x; v.w[1] = w.y;
-  } else {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
-    v.w[0] = w.x; v.w[1] = w.y; v.w[2] = w.z; v.w[3] = w.w;
   }
+  return v;
 }
 template <typename T>
-__device__ __forceinline__ void store_piece(const float2 (&f)[2], char* p) {
+__device__ __forceinline__ void store_piece(float2 f, char* p) {
   RowVec<T, VEC> v;
-  const float flat[4] = {f[0].x, f[0].y, f[1].x, f[1].y};
+  const float flat[2] = {f.x, f.y};
   v.set(flat);
   v.store(reinterpret_cast<T*>(p));
 }
 template <typename T>
-__device__ __forceinline__ float2 pair(const RowVec<T, VEC>& v, int j) { return make_float2(v.get(2 * j), v.get(2 * j + 1)); }
+__device__ __forceinline__ float2 pair(const RowVec<T, VEC>& v) { return make_float2(v.get(0), v.get(1)); }
 __device__ __forceinline__ float2 closed_step(float2 a, float2 s, float2 x) {
   return make_float2(rec_step(a.x, s.x, x.x), rec_step(a.y, s.y, x.y));
 }
 __device__ __forceinline__ float2 unless_closed(float2 a, float2 v) { return make_float2(a.x == 0.f ? 0.f : v.x, a.y == 0.f ? 0.f : v.y); }
+
+// exp of the log-gates.  From -4 up, 2^(x log2 e) with one rounding of the exponent, which is off by 2^-22 there, and the power by 2^-22
+// of itself; below, where the rounded exponent would cost more, expf.
+template <typename T, int STEPS>
+__device__ __forceinline__ void open_gates(const RowVec<T, VEC> (&a)[STEPS], float2 (&gate)[STEPS]) {
+  bool near;
+  if constexpr (sizeof(T) == 2) {
+    __nv_bfloat162 least = __floats2bfloat162_rn(0.f, 0.f);
+#pragma unroll
+    for (int l = 0; l < STEPS; ++l) least = __hmin2(least, *reinterpret_cast<const __nv_bfloat162*>(&a[l].w[0]));
+    near = fminf(__low2float(least), __high2float(least)) >= -4.f;
+  } else {
+    float least = 0.f;
+#pragma unroll
+    for (int l = 0; l < STEPS; ++l) least = fminf(least, fminf(a[l].get(0), a[l].get(1)));
+    near = least >= -4.f;
+  }
+  if (near) {
+#pragma unroll
+    for (int l = 0; l < STEPS; ++l) {
+      gate[l] = __fmul2_rn(pair(a[l]), make_float2(1.4426950408889634f, 1.4426950408889634f));
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(gate[l].x));
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(gate[l].y));
+    }
+  } else {
+#pragma unroll
+    for (int l = 0; l < STEPS; ++l) gate[l] = make_float2(expf(a[l].get(0)), expf(a[l].get(1)));
+  }
+}
 
 struct Maps {
   CUtensorMap x, log_a, h, out, dlog_a;
@@ -97,17 +133,20 @@ struct Maps {
 
 template <typename TX, typename TA, int STEPS, int STAGES, bool BACK>
 __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __grid_constant__ Maps maps, const float* begin, const float* h0,
-                                                                        float* end, int64_t T, int channels) {
+                                                                        float* end, int T, int channels) {
   using Shape = Tile<TX, TA, STEPS, BACK>;
-  static_assert(STAGES >= 3, "a round's tile is asked for in an earlier round");
+  static_assert(STAGES >= 4, "a round's tile is asked for two rounds before its map is formed, one round ahead");
+  static_assert(REC_THREADS == 4 * COLS && 32 * VEC == COLS, "half of the threads join the states of a channel, half send its map");
   extern __shared__ __align__(128) char stages[];
-  __shared__ __align__(16) float2 warp_map[REC_WARPS][COLS];                  // (A, H) of a warp's tokens
-  __shared__ __align__(16) float entering[REC_WARPS][COLS];                   // the state that enters a warp's tokens
+  __shared__ __align__(16) float2 warp_map[2][REC_WARPS][COLS];      // (A, H) of a warp's tokens, of this round and of the next
+  __shared__ __align__(16) float entering[2][REC_WARPS][COLS];       // the state that enters a warp's tokens
   __shared__ __align__(8) float2 tile_map[2][REC_MAX_CLUSTER][COLS];
   __shared__ uint64_t full[STAGES], maps_in[2];
   const cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, column = lane % LANES, part = tid / LANES;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int channel = tid % COLS, half = tid / COLS & 1;      // whose states (the first 128 threads) or maps this thread joins
+  const bool joins = tid < 2 * COLS;
   const int b = blockIdx.z, c0 = blockIdx.y * COLS;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) tc::mbar_init(&full[i], 1);
@@ -115,17 +154,15 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     tc::mbar_init(&maps_in[1], 1);
     tc::fence_barrier_init();
   }
-  pdl_trigger();
   if (ranks > 1) cluster.sync();      // all of the cluster run, with their barriers ready, before one sends to another
   else __syncthreads();
   pdl_wait();
-  const int64_t tiles = (T + Shape::TOKENS - 1) / Shape::TOKENS;
-  const int rounds = (int)((tiles + ranks - 1) / ranks);
-  // this CTA's tile of a round, by its place in the order of the recurrence; none from `tiles` on
-  const auto turn_of = [&](int round) { return (int64_t)round * ranks + rank; };
-  const auto token_of = [&](int round) { return (int)((BACK ? tiles - 1 - turn_of(round) : turn_of(round)) * Shape::TOKENS); };
+  const int tiles = (T + Shape::TOKENS - 1) / Shape::TOKENS, rounds = (tiles + ranks - 1) / ranks;
+  // this CTA's tile of a round is number round * ranks + rank in the order of the recurrence; the last round may have none for it
+  const int own_rounds = (tiles - rank + ranks - 1) / ranks;
+  const auto token_of = [&](int round) { return (BACK ? tiles - 1 - (round * ranks + rank) : round * ranks + rank) * Shape::TOKENS; };
   const auto fetch = [&](int round) {
-    if (round >= rounds || turn_of(round) >= tiles) return;
+    if (round >= own_rounds) return;
     char* to = stages + (round % STAGES) * Shape::BYTES;
     uint64_t* bar = &full[round % STAGES];
     const int t = token_of(round);
@@ -135,7 +172,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     if (BACK) tc::tma_load_3d(to + Shape::H_AT, &maps.h, c0, t - 1, b, bar);
   };
   const auto put = [&](int round) {      // the outputs of a round, once all threads have written them
-    if (turn_of(round) < tiles) {
+    if (round < own_rounds) {
       const char* from = stages + (round % STAGES) * Shape::BYTES;
       store_tile(&maps.out, from, c0, token_of(round), b);
       if (BACK) store_tile(&maps.dlog_a, from + Shape::A_AT, c0, token_of(round), b);
@@ -145,84 +182,144 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   if (tid == PORTER)
     for (int r = 0; r < STAGES; ++r) fetch(r);
 
-  const bool joins = tid < COLS, mine = joins && c0 + tid < channels;
+  const bool mine = c0 + channel < channels;
   const int64_t row = (int64_t)b * channels + c0;
-  float carry = mine && begin ? begin[row + tid] : 0.f;
+  float carry = joins && mine && begin ? begin[row + channel] : 0.f;
   bool lost = false;
-  // offset of this thread's first token (in the order of the recurrence) in a tile, and from one to the next
-  const int place = BACK ? Shape::TOKENS - 1 - part * STEPS : part * STEPS;
+  // this thread's first token (in the order of the recurrence) in a tile, and from one to the next
+  const int place = (BACK ? Shape::TOKENS - 1 - warp * STEPS : warp * STEPS) * COLS + lane * VEC;
   constexpr int WAY = BACK ? -COLS : COLS;
-  for (int round = 0; round < rounds; ++round) {
-    const bool here = turn_of(round) < tiles;
-    char* stage = stages + (round % STAGES) * Shape::BYTES;
-    char* xs = stage + (place * COLS + column * VEC) * sizeof(TX);
-    char* as = stage + Shape::A_AT + (place * COLS + column * VEC) * sizeof(TA);
-    const char* hs = stage + Shape::H_AT + (place * COLS + column * VEC) * sizeof(TX);
+
+  // A thread's tokens of a round: gates and rows from the time that their map is formed until they are gone over again.
+  struct Tokens {
+    float2 gate[STEPS];
     RowVec<TX, VEC> x[STEPS];
-    float2 gate[STEPS][2], A[2], H[2];
-    A[0] = A[1] = make_float2(1.f, 1.f);
-    H[0] = H[1] = make_float2(0.f, 0.f);
-    if (here) {
-      wait(&full[round % STAGES], (round / STAGES) & 1, lost);
-      float least = 0.f;
+  };
+  const auto form = [&](int round, int stage, uint32_t phase, Tokens& k) {
+    float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+    if (round < own_rounds) {
+      wait(&full[stage], phase, lost);
+      const char* xs = stages + stage * Shape::BYTES + place * sizeof(TX);
+      const char* as = stages + stage * Shape::BYTES + Shape::A_AT + place * sizeof(TA);
       RowVec<TA, VEC> a[STEPS];
 #pragma unroll
       for (int l = 0; l < STEPS; ++l) {
-        load_piece(x[l], xs + l * WAY * (int)sizeof(TX));
-        load_piece(a[l], as + l * WAY * (int)sizeof(TA));
+        a[l] = load_piece<TA>(as + l * WAY * (int)sizeof(TA));
+        k.x[l] = load_piece<TX>(xs + l * WAY * (int)sizeof(TX));
       }
-      // exp: from -4 up, 2^(x log2 e) with one rounding of the exponent, which is off by 2^-22 there, and the power by 2^-22 of
-      // itself; below, where the rounded exponent would cost more, expf
+      open_gates(a, k.gate);
 #pragma unroll
-      for (int l = 0; l < STEPS; ++l)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 v = pair(a[l], j);
-          least = fminf(least, fminf(v.x, v.y));
-          gate[l][j] = __fmul2_rn(v, make_float2(1.4426950408889634f, 1.4426950408889634f));
-          asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(gate[l][j].x));
-          asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(gate[l][j].y));
-        }
-      if (!(least >= -4.f)) {
+      for (int l = 0; l < STEPS; ++l) {
+        A = __fmul2_rn(A, k.gate[l]);
+        H = BACK ? __fmul2_rn(k.gate[l], __fadd2_rn(H, pair(k.x[l]))) : __ffma2_rn(k.gate[l], H, pair(k.x[l]));
+      }
+      if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) {
+        H = make_float2(0.f, 0.f);
 #pragma unroll
         for (int l = 0; l < STEPS; ++l)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) gate[l][j] = make_float2(expf(a[l].get(2 * j)), expf(a[l].get(2 * j + 1)));
+          H = BACK ? unless_closed(k.gate[l], __fmul2_rn(k.gate[l], __fadd2_rn(H, pair(k.x[l])))) : closed_step(k.gate[l], H, pair(k.x[l]));
       }
-      // the map of this thread's tokens
+      if (lost) H = make_float2(NAN, NAN);
+    }
+    *reinterpret_cast<float4*>(&warp_map[round & 1][warp][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
+  };
+  // The second 128 threads send this CTA's map of a round to all ranks, every other one each.
+  uint32_t to[REC_MAX_CLUSTER / 2], bar_in[REC_MAX_CLUSTER / 2];
 #pragma unroll
-      for (int l = 0; l < STEPS; ++l)
+  for (int i = 0; i < REC_MAX_CLUSTER / 2; ++i) {
+    const int r = 2 * i + half < ranks ? 2 * i + half : rank;
+    to[i] = in_rank(&tile_map[0][rank][channel], r);
+    bar_in[i] = in_rank(&maps_in[0], r);
+  }
+  const auto publish = [&](int round) {
+    if (joins || ranks == 1) return;
+    const int turn = round & 1;
+    float2 m = warp_map[turn][0][channel];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          A[j] = __fmul2_rn(A[j], gate[l][j]);
-          H[j] = BACK ? __fmul2_rn(gate[l][j], __fadd2_rn(H[j], pair(x[l], j))) : __ffma2_rn(gate[l][j], H[j], pair(x[l], j));
+    for (int w = 1; w < REC_WARPS; ++w) {
+      const float2 n = warp_map[turn][w][channel];
+      m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
+    }
+    if (tid == PORTER) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
+#pragma unroll
+    for (int i = 0; i < REC_MAX_CLUSTER / 2; ++i)
+      if (2 * i + half < ranks) send(to[i] + turn * (uint32_t)sizeof(tile_map[0]), bar_in[i] + turn * 8u, m);
+  };
+  // The first 128 form the states that enter the warps' tokens, four each; the maps of a round have been on their way for a round.
+  const auto enter = [&](int round) {
+    if (!joins) return;
+    const int turn = round & 1;
+    float state = carry;
+    if (ranks > 1) {
+      wait_sent(&maps_in[turn], (round >> 1) & 1, lost);
+      float behind = carry;
+#pragma unroll
+      for (int r = 0; r < REC_MAX_CLUSTER; ++r) {
+        if (r >= ranks) break;
+        if (r == rank) state = behind;
+        const float2 m = tile_map[turn][r][channel];
+        behind = rec_step(m.x, behind, m.y);
+      }
+      carry = behind;
+      if (lost) state = carry = NAN;
+    }
+#pragma unroll
+    for (int w = 0; w < REC_WARPS; ++w) {
+      if (w / (REC_WARPS / 2) == half) entering[turn][w][channel] = state;
+      const float2 m = warp_map[turn][w][channel];
+      state = rec_step(m.x, state, m.y);
+    }
+    if (ranks == 1) carry = state;
+  };
+  // A round's tokens again, from the state that enters them.
+  const auto apply = [&](int round, char* stage, const Tokens& k) {
+    if (round >= own_rounds) return;
+    char* xs = stage + place * sizeof(TX);
+    char* as = stage + Shape::A_AT + place * sizeof(TA);
+    const char* hs = stage + Shape::H_AT + place * sizeof(TX);
+    const float2 from = *reinterpret_cast<const float2*>(&entering[round & 1][warp][lane * VEC]);
+    const bool first = BACK && token_of(round) == 0 && warp == REC_WARPS - 1;      // token 0 is this thread's last
+    const auto go = [&](auto closed) {
+      constexpr bool CLOSED = decltype(closed)::value;
+      const float2 none = make_float2(0.f, 0.f);
+      float2 s = from, zeros = none;
+#pragma unroll
+      for (int l = 0; l < STEPS; ++l) {
+        const float2 a = k.gate[l];
+        if constexpr (BACK) {
+          const float2 v = __fadd2_rn(pair(k.x[l]), s);                // dx
+          s = __fmul2_rn(a, v);                                        // c
+          if (CLOSED) s = unless_closed(a, s);
+          float2 before = pair(load_piece<TX>(hs + l * WAY * (int)sizeof(TX)));
+          if (l == STEPS - 1 && first && h0) {
+            const int c = lane * VEC;
+            before = make_float2(c0 + c < channels ? h0[row + c] : 0.f, c0 + c + 1 < channels ? h0[row + c + 1] : 0.f);
+          }
+          float2 d = __fmul2_rn(s, before);
+          if (CLOSED) d = unless_closed(a, d);
+          else zeros = __ffma2_rn(d, none, zeros);
+          store_piece<TX>(v, xs + l * WAY * (int)sizeof(TX));
+          store_piece<TA>(d, as + l * WAY * (int)sizeof(TA));
+        } else {
+          s = CLOSED ? closed_step(a, s, pair(k.x[l])) : __ffma2_rn(a, s, pair(k.x[l]));
+          store_piece<TX>(s, xs + l * WAY * (int)sizeof(TX));
         }
-      const float zeros = fmaf(H[0].x, 0.f, fmaf(H[0].y, 0.f, fmaf(H[1].x, 0.f, H[1].y * 0.f)));
-      if (rec_not_finite(zeros)) {
-        H[0] = H[1] = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int l = 0; l < STEPS; ++l)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            H[j] = BACK ? unless_closed(gate[l][j], __fmul2_rn(gate[l][j], __fadd2_rn(H[j], pair(x[l], j))))
-                        : closed_step(gate[l][j], H[j], pair(x[l], j));
       }
-      if (lost) H[0] = H[1] = make_float2(NAN, NAN);
-    }
-    // ... of the other half's tokens before them, and of all of the warp's
-    float2 before_A[2], before_H[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float2 a = make_float2(__shfl_up_sync(0xffffffffu, A[j].x, 16), __shfl_up_sync(0xffffffffu, A[j].y, 16));
-      const float2 h = make_float2(__shfl_up_sync(0xffffffffu, H[j].x, 16), __shfl_up_sync(0xffffffffu, H[j].y, 16));
-      before_A[j] = lane < 16 ? make_float2(1.f, 1.f) : a;
-      before_H[j] = lane < 16 ? make_float2(0.f, 0.f) : h;
-      if (lane >= 16) {
-        H[j] = closed_step(A[j], h, H[j]);
-        A[j] = __fmul2_rn(A[j], a);
-        *reinterpret_cast<float4*>(&warp_map[warp][column * VEC + 2 * j]) = make_float4(A[j].x, H[j].x, A[j].y, H[j].y);
-      }
-    }
+      zeros = __ffma2_rn(s, none, zeros);
+      return zeros.x + zeros.y;
+    };
+    if (rec_not_finite(go(std::false_type()))) go(std::true_type());
+    tc::fence_proxy_async();      // seen by the copy that takes the tile away
+  };
+  // the stage of the round whose tokens are gone over, and the parity in which the next one's tile comes
+  int at = 0;
+  uint32_t phase = 0;
+  const auto step = [&](int round, const Tokens& now, Tokens& next) {
+    char* stage = stages + at * Shape::BYTES;
+    at = at + 1 == STAGES ? 0 : at + 1;
+    phase ^= at == 0;
+    enter(round);
+    if (round + 1 < rounds) form(round + 1, at, phase, next);
     __syncthreads();
     if (tid == PORTER && round > 0) {
       put(round - 1);
@@ -231,90 +328,30 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
         fetch(round - 2 + STAGES);
       }
     }
-    if (joins) {
-      const int turn = round & 1;
-      if (ranks > 1) {
-        float2 m = warp_map[0][tid];
-#pragma unroll
-        for (int w = 1; w < REC_WARPS; ++w) {
-          const float2 n = warp_map[w][tid];
-          m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
-        }
-        if (tid == 0) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
-        for (int r = 0; r < ranks; ++r) send(&tile_map[turn][rank][tid], r, &maps_in[turn], m);
-        wait_sent(&maps_in[turn], (round >> 1) & 1, lost);
-        if (lost) carry = NAN;
-      }
-      float state = carry, behind = carry;
-      if (ranks > 1) {
-        for (int r = 0; r < ranks; ++r) {
-          if (r == rank) state = behind;
-          const float2 m = tile_map[turn][r][tid];
-          behind = rec_step(m.x, behind, m.y);
-        }
-      }
-#pragma unroll
-      for (int w = 0; w < REC_WARPS; ++w) {
-        entering[w][tid] = state;
-        const float2 m = warp_map[w][tid];
-        state = rec_step(m.x, state, m.y);
-      }
-      carry = ranks > 1 ? behind : state;
-    }
-    __syncthreads();
-    if (!here) continue;
-    // the tokens again, from the state that enters them
-    const float4 e = *reinterpret_cast<const float4*>(&entering[warp][column * VEC]);
-    float2 state[2] = {closed_step(before_A[0], make_float2(e.x, e.y), before_H[0]), closed_step(before_A[1], make_float2(e.z, e.w), before_H[1])};
-    const bool first = BACK && token_of(round) == 0 && part == PARTS - 1;      // token 0 is this thread's last
-    const auto go = [&](auto closed) {
-      constexpr bool CLOSED = decltype(closed)::value;
-      float2 s[2] = {state[0], state[1]}, zeros = make_float2(0.f, 0.f);
-      const float2 none = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int l = 0; l < STEPS; ++l) {
-        float2 v[2], d[2];
-        RowVec<TX, VEC> h;
-        if (BACK) load_piece(h, hs + l * WAY * (int)sizeof(TX));
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float2 a = gate[l][j];
-          if (BACK) {
-            v[j] = __fadd2_rn(pair(x[l], j), s[j]);                      // dx
-            s[j] = __fmul2_rn(a, v[j]);                                  // c
-            if (CLOSED) s[j] = unless_closed(a, s[j]);
-            float2 before = pair(h, j);
-            if (l == STEPS - 1 && first && h0) {
-              const int c = column * VEC + 2 * j;
-              before = make_float2(c0 + c < channels ? h0[row + c] : 0.f, c0 + c + 1 < channels ? h0[row + c + 1] : 0.f);
-            }
-            d[j] = __fmul2_rn(s[j], before);
-            if (CLOSED) d[j] = unless_closed(a, d[j]);
-            else zeros = __ffma2_rn(d[j], none, zeros);
-          } else {
-            v[j] = s[j] = CLOSED ? closed_step(a, s[j], pair(x[l], j)) : __ffma2_rn(a, s[j], pair(x[l], j));
-          }
-        }
-        store_piece<TX>(v, xs + l * WAY * (int)sizeof(TX));
-        if constexpr (BACK) store_piece<TA>(d, as + l * WAY * (int)sizeof(TA));
-      }
-      zeros = __ffma2_rn(s[0], none, __ffma2_rn(s[1], none, zeros));
-      return zeros.x + zeros.y;
-    };
-    if (rec_not_finite(go(std::false_type()))) go(std::true_type());
-    tc::fence_proxy_async();      // seen by the copy that takes the tile away
+    if (round + 1 < rounds) publish(round + 1);
+    apply(round, stage, now);
+  };
+
+  Tokens even, odd;
+  form(0, 0, 0, even);
+  __syncthreads();
+  publish(0);
+  for (int round = 0; round < rounds; round += 2) {
+    step(round, even, odd);
+    if (round + 1 < rounds) step(round + 1, odd, even);
   }
+  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
   __syncthreads();
   if (tid == PORTER) {
     put(rounds - 1);
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     // copies that were waited for in vain land before the CTA leaves, or not within the limit
-    for (int r = rounds > STAGES ? rounds - STAGES : 0; lost && r < rounds; ++r) {
+    for (int r = rounds > STAGES ? rounds - STAGES : 0; lost && r < own_rounds; ++r) {
       bool late = false;
-      if (turn_of(r) < tiles) wait(&full[r % STAGES], (r / STAGES) & 1, late);
+      wait(&full[r % STAGES], (r / STAGES) & 1, late);
     }
   }
-  if (end && rank == 0 && mine) end[row + tid] = carry;
+  if (end && rank == 0 && mine && tid < COLS) end[row + tid] = carry;
 }
 
 template <typename TX, typename TA, int STEPS, int STAGES, bool BACK>
@@ -335,7 +372,7 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   const int64_t columns = (a.channels + COLS - 1) / COLS, tiles = (a.T + Shape::TOKENS - 1) / Shape::TOKENS;
   const unsigned ranks = rec_ranks(columns, batch, tiles);
   return smat_launch_pdl_cluster(kernel, dim3(ranks, (unsigned)columns, (unsigned)batch), REC_THREADS, bytes, ranks, st, maps, a.begin, a.h0, a.end,
-                                 a.T, a.channels);
+                                 (int)a.T, a.channels);
 }
 
 }  // namespace
@@ -355,7 +392,7 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
 // Stages and tokens of a tile: two CTAs an SM, with two tiles or more on their way.
 cudaError_t smat_launch_recurrence_tma(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back, cudaStream_t st) {
   using bf16 = __nv_bfloat16;
-  if (!x_bf16) return back ? launch<float, float, 2, 4, true>(a, batch, st) : launch<float, float, 4, 3, false>(a, batch, st);
-  if (gate_bf16) return back ? launch<bf16, bf16, 4, 4, true>(a, batch, st) : launch<bf16, bf16, 8, 3, false>(a, batch, st);
-  return back ? launch<bf16, float, 4, 3, true>(a, batch, st) : launch<bf16, float, 4, 4, false>(a, batch, st);
+  if (!x_bf16) return back ? launch<float, float, 2, 7, true>(a, batch, st) : launch<float, float, 4, 5, false>(a, batch, st);
+  if (gate_bf16) return back ? launch<bf16, bf16, 4, 7, true>(a, batch, st) : launch<bf16, bf16, 8, 5, false>(a, batch, st);
+  return back ? launch<bf16, float, 4, 5, true>(a, batch, st) : launch<bf16, float, 4, 7, false>(a, batch, st);
 }
