@@ -5,11 +5,13 @@
 
 namespace {
 
+// Threads an SM holds: what the registers allow.
+__host__ __device__ constexpr int norm_resident(int mode) { return mode == NORM_ANY ? 768 : 1024; }
 // Operands a kernel reads: the rows, the residual, the gate.
 __host__ __device__ constexpr int norm_operands(int mode) { return mode == NORM_ROWS ? 1 : mode == NORM_ANY ? 3 : 2; }
 
 template <typename T, int VEC, int E, int THREADS, int MODE>
-__global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, norm_resident(MODE) / THREADS) norm_forward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
   constexpr bool ANY = MODE == NORM_ANY;
   __shared__ float exchange[2][32][1];
@@ -21,7 +23,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) norm_forward_kernel(co
   const int lane = threadIdx.x % a.lanes, column = lane * VEC, apart = a.lanes * VEC;
   NormWalk at(a);
   pdl_wait();
-  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
+  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, 8, THREADS);
   constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
   extern __shared__ uint4 rows_shared[];
   NormRing<N, DEPTH> ring(rows_shared);
@@ -135,8 +137,9 @@ cudaError_t launch(NormArgs& a, const NormShape& s, cudaStream_t st) {
   a.lanes = s.lanes;
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   // as many CTAs as run at once, a group's share of them each, but none without a row
-  norm_walk(&a, slots, (uint32_t)NORM_SMS * (threads > 512 ? 1 : 768 / threads) / a.groups);
-  return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, THREADS,
+  norm_walk(&a, slots, (uint32_t)(NORM_SMS * norm_ctas_an_sm(norm_resident(MODE), threads)) / a.groups);
+  return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 8, THREADS,
+                     norm_ctas_an_sm(norm_resident(MODE), threads),
                      dim3(a.ctas * a.groups), threads, st, a);
 }
 

@@ -119,10 +119,10 @@ struct NormRing {
 };
 // Whether a row of `operands` pieces a thread has room in shared memory (fp32 rows of more than 8192 columns do not).
 __host__ __device__ constexpr bool norm_rings(int operands, int threads) { return operands * threads * 16 <= 160 * 1024; }
-// Rows on their way for a thread: 8 pieces of 16 bytes of two operands (the forward pass of small calls: no more than every
-// kernel may take, asking for more costs a call of the runtime), 16 of more.
-__host__ __device__ constexpr int norm_depth(int operands, int threads) {
-  const int depth = (threads > 512 ? 8 : operands == 2 ? 8 : 16) / operands;
+// Rows on their way for a thread that has room for so many pieces of 16 bytes (the forward pass 8: with four CTAs an SM, and so that
+// small calls take no more shared memory than every kernel may, asking for more costs a call of the runtime; the backward pass 16).
+__host__ __device__ constexpr int norm_depth(int operands, int pieces, int threads) {
+  const int depth = (threads > 512 ? 8 : pieces) / operands;
   return depth > 5 ? 5 : depth < 1 ? 1 : depth;
 }
 
@@ -174,11 +174,17 @@ inline void norm_walk(NormArgs* a, uint32_t slots, uint32_t ctas) {
   }
 }
 
-// A launch with a ring of `operands` pieces a row (none: 0) for each of its threads.
+inline int norm_ctas_an_sm(int resident, uint32_t threads) { return threads >= (uint32_t)resident ? 1 : resident / (int)threads; }
+
+// A launch with a ring of `operands` pieces a row (none: 0) for each of its threads.  CTAs walk over the rows, so that each SM has to
+// get as many of them: they ask for so much shared memory that no more fit.  (Where a fourth one fitted beside three, SMs that
+// drained early took four of the next launch and left others with two: the gated norm of heads took 167 us for 132.)
 template <typename Kernel>
-cudaError_t norm_launch(Kernel kernel, int operands, int most_threads, dim3 grid, uint32_t threads, cudaStream_t st, const NormArgs& a) {
-  const size_t bytes = operands && norm_rings(operands, most_threads) ? (size_t)norm_depth(operands, most_threads) * operands * threads * 16 : 0;
-  if (bytes > 36 * 1024) {      // (with what a kernel has besides, more than every kernel may take)
+cudaError_t norm_launch(Kernel kernel, int operands, int pieces, int most_threads, int an_sm, dim3 grid, uint32_t threads, cudaStream_t st, const NormArgs& a) {
+  size_t bytes = operands && norm_rings(operands, most_threads) ? (size_t)norm_depth(operands, pieces, most_threads) * operands * threads * 16 : 0;
+  const size_t no_more = (size_t)228 * 1024 / (an_sm + 1) - 1024 + 256;
+  if (bytes < no_more && an_sm > 2) bytes = no_more;
+  if (bytes + (pieces > 8 ? 9216 : 512) > 48 * 1024) {      // (with the sums and exchanges that a kernel has besides)
     const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (err != cudaSuccess) return err;
   }

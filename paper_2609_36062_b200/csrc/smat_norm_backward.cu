@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
   NormWalk at(a);
   const uint32_t slots = at.slots, slot = at.slot;
   pdl_wait();
-  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, THREADS);
+  constexpr int N = norm_operands(MODE) * VPT, DEPTH = norm_depth(N, 16, THREADS);
   constexpr bool RING = VEC * sizeof(T) == 16 && norm_rings(N, THREADS);
   constexpr int X = 3 * VPT, Z = (ANY ? 4 : 3) * VPT;      // places of the branch's rows and of the gate
   extern __shared__ uint4 rows_shared[];
@@ -252,8 +252,8 @@ cudaError_t launch(NormArgs& a, const NormShape& s, float* dw, float* ds, cudaSt
   a.lanes = s.lanes;
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   norm_walk(&a, slots, (uint32_t)smat_norm_partials((int)a.groups, a.width) / a.groups);
-  cudaError_t err = norm_launch(norm_backward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0,
-                                THREADS, dim3(a.ctas * a.groups), threads, st, a);
+  cudaError_t err = norm_launch(norm_backward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 16,
+                                THREADS, norm_ctas_an_sm(512, threads), dim3(a.ctas * a.groups), threads, st, a);
   if (err != cudaSuccess || (!dw && !ds)) return err;
   const int grouped = a.weight_group ? 1 : 0;
   const dim3 grid((unsigned)((a.width + SUM_COLS - 1) / SUM_COLS), ds ? 2u : 1u, grouped ? a.groups : 1u);
@@ -284,7 +284,7 @@ cudaError_t moded(NormArgs& a, float* dw, float* ds, cudaStream_t st) {
 int smat_norm_partials(int groups, int width) {
   const NormShape s = norm_shape(width);
   const int threads = s.lanes <= 32 ? 256 : s.lanes;
-  const int all = NORM_SMS * (threads > 512 ? 1 : 512 / threads);
+  const int all = NORM_SMS * norm_ctas_an_sm(512, threads);
   return all > groups ? all / groups * groups : groups;
 }
 
