@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int ROT_THREADS = 256, ROT_UNROLL = 4;
-constexpr uint32_t ROT_CTAS = 148 * 8;   // as many as run at once
+constexpr uint32_t ROT_CTAS = 148 * 4 * 6;   // six times as many as run at once
 
 struct RotaryArgs {
   const void* x[2];
