@@ -514,27 +514,22 @@ class SmatPlan:
 
     def decode_pack(self, cache, packed=None, stream=None) -> torch.Tensor:
         """smat_decode_pack: the packed form of a decode cache."""
-        self._check_bytes(cache, "cache")
         packed = self.decode_cache_packed(cache.device) if packed is None else packed
-        self._check_bytes(packed, "packed")
-        _check(self.lib.smat_decode_pack(self.handle, _ptr(cache), cache.numel(), _ptr(packed), packed.numel(), _stream(stream)),
-               "smat_decode_pack")
+        self._native.repack(cache, packed, stream, True)
         return packed
 
     def decode_unpack(self, packed, cache=None, stream=None) -> torch.Tensor:
         """smat_decode_unpack: the decode cache that a packed one stands for."""
-        self._check_bytes(packed, "packed")
         cache = self.decode_cache(packed.device) if cache is None else cache
-        self._check_bytes(cache, "cache")
-        _check(self.lib.smat_decode_unpack(self.handle, _ptr(packed), packed.numel(), _ptr(cache), cache.numel(), _stream(stream)),
-               "smat_decode_unpack")
+        self._native.repack(cache, packed, stream, False)
         return cache
 
     def decode_begin_packed(self, K, V, packed, log_a=None, workspace=None, stream=None) -> None:
         """smat_decode_begin_packed; log_a [batch*heads, T] on gated plans."""
         _, _, _, dk, dv = self.shape
         self._check_tensor(K, dk, "K"); self._check_tensor(V, dv, "V")
-        self._check_bytes(packed, "packed")
+        if not (packed.is_cuda and packed.dtype == torch.uint8 and packed.is_contiguous()):
+            raise ValueError("packed: expected a contiguous CUDA uint8 tensor")
         if log_a is not None:
             self._check_gates(log_a)
         ws = self.workspace(False, K.device) if workspace is None else workspace
@@ -545,11 +540,6 @@ class SmatPlan:
     def decode_step_packed(self, q, k, v, t: int, packed, log_a_t=None, o=None, stream=None):
         """smat_decode_step_packed; log_a_t, the token's log-gates, on gated plans."""
         return self._native.decode_step(q, k, v, log_a_t, t, packed, o, stream, True)
-
-    @staticmethod
-    def _check_bytes(t: torch.Tensor, name: str) -> None:
-        if not (t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()):
-            raise ValueError(f"{name}: expected a contiguous CUDA uint8 tensor")
 
     # -- verification exports ------------------------------------------------------------------
     def routing_indices(self):

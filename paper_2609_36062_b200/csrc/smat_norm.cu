@@ -6,12 +6,12 @@
 namespace {
 
 // Threads an SM holds: what the registers allow.
-__host__ __device__ constexpr int norm_resident(int mode) { return mode == NORM_ANY ? 768 : 1024; }
+__host__ __device__ constexpr int norm_resident(int mode, int columns) { return mode == NORM_ANY || columns > 8 ? 768 : 1024; }
 // Operands a kernel reads: the rows, the residual, the gate.
 __host__ __device__ constexpr int norm_operands(int mode) { return mode == NORM_ROWS ? 1 : mode == NORM_ANY ? 3 : 2; }
 
 template <typename T, int VEC, int E, int THREADS, int MODE>
-__global__ void __launch_bounds__(THREADS, norm_resident(MODE) / THREADS) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, norm_resident(MODE, E) >= THREADS ? norm_resident(MODE, E) / THREADS : 1) norm_forward_kernel(const NormArgs a) {
   constexpr int VPT = E / VEC;
   constexpr bool ANY = MODE == NORM_ANY;
   __shared__ float exchange[2][32][1];
@@ -137,28 +137,38 @@ cudaError_t launch(NormArgs& a, const NormShape& s, cudaStream_t st) {
   a.lanes = s.lanes;
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   // as many CTAs as run at once, a group's share of them each, but none without a row
-  norm_walk(&a, slots, (uint32_t)(NORM_SMS * norm_ctas_an_sm(norm_resident(MODE), threads)) / a.groups);
+  norm_walk(&a, slots, (uint32_t)(NORM_SMS * norm_ctas_an_sm(norm_resident(MODE, E), threads)) / a.groups);
   return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 8, THREADS,
-                     norm_ctas_an_sm(norm_resident(MODE), threads),
+                     norm_ctas_an_sm(norm_resident(MODE, E), threads),
                      dim3(a.ctas * a.groups), threads, st, a);
 }
 
 template <typename T, int VEC, int MODE>
 cudaError_t shaped(NormArgs& a, cudaStream_t st) {
-  const NormShape s = norm_shape(a.width);
+  constexpr bool WHOLE = VEC * sizeof(T) == 16, ROOMY = WHOLE && (MODE == NORM_ROWS || MODE == NORM_STREAM);
+  const NormShape s = norm_shape(a.width, ROOMY);
+  constexpr int WIDE = WHOLE ? MODE : NORM_ANY;      // (rows of single elements or pairs: one kernel for all long ones)
+  if (s.columns == 16) {
+    if constexpr (ROOMY) {
+      if (s.threads == 256) return launch<T, VEC, 16, 256, MODE>(a, s, st);
+      if (s.threads == 512) return launch<T, VEC, 16, 512, MODE>(a, s, st);
+    }
+    return launch<T, VEC, 16, 1024, WIDE>(a, s, st);
+  }
   if (s.threads == 256) return launch<T, VEC, 8, 256, MODE>(a, s, st);
-  if (s.threads == 512) return launch<T, VEC, 8, 512, MODE>(a, s, st);
-  return s.columns == 8 ? launch<T, VEC, 8, 1024, MODE>(a, s, st) : launch<T, VEC, 16, 1024, MODE>(a, s, st);
+  if constexpr (!ROOMY) {
+    if (s.threads == 512) return launch<T, VEC, 8, 512, MODE>(a, s, st);
+    return s.threads == 768 ? launch<T, VEC, 8, 768, WIDE>(a, s, st) : launch<T, VEC, 8, 1024, WIDE>(a, s, st);
+  }
+  return cudaErrorInvalidValue;
 }
 
 template <typename T, int VEC>
 cudaError_t moded(NormArgs& a, cudaStream_t st) {
-  if constexpr (VEC > 2) {
-    if (!a.gate.data && a.residual.data) return shaped<T, VEC, NORM_STREAM>(a, st);
-    if (!a.residual.data && !a.scale && !a.h.data) {
-      if (!a.gate.data) return shaped<T, VEC, NORM_ROWS>(a, st);
-      return a.sigmoid ? shaped<T, VEC, NORM_SIGMOID>(a, st) : shaped<T, VEC, NORM_SILU>(a, st);
-    }
+  if (!a.gate.data && a.residual.data) return shaped<T, VEC, NORM_STREAM>(a, st);
+  if (!a.residual.data && !a.scale && !a.h.data) {
+    if (!a.gate.data) return shaped<T, VEC, NORM_ROWS>(a, st);
+    return a.sigmoid ? shaped<T, VEC, NORM_SIGMOID>(a, st) : shaped<T, VEC, NORM_SILU>(a, st);
   }
   return shaped<T, VEC, NORM_ANY>(a, st);
 }

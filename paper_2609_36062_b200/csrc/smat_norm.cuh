@@ -139,26 +139,27 @@ __device__ __forceinline__ void norm_row_sum(float (&v)[N], int lanes, int turn,
 #pragma unroll
     for (int i = 0; i < N; ++i) part[turn & 1][threadIdx.x >> 5][i] = v[i];
   __syncthreads();
+  const int all = warps > 16 ? 32 : warps > 8 ? 16 : warps > 4 ? 8 : warps > 2 ? 4 : 2, other = lane & (all - 1);
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = part[turn & 1][lane & (warps - 1)][i];
-  for (int o = warps / 2; o > 0; o >>= 1)
+  for (int i = 0; i < N; ++i) v[i] = other < warps ? part[turn & 1][other][i] : 0.f;
+  for (int o = all / 2; o > 0; o >>= 1)
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
-// Columns a lane holds, the CTA's threads at most and the lanes, by the width alone.  Eight columns a lane as long as a CTA holds
-// the row with them: at 128 registers a thread of the backward pass keeps its row, the next one and the sums of dw and dscale
-// there without spills (sixteen columns spilled 800 bytes), and 512 threads an SM have enough on its way.
+// Columns a lane holds, the CTA's threads at most and the lanes, by the width: a power of two up to a warp, then whole warps.  Sixteen
+// columns where a kernel has registers for them (`roomy`) and the row is longer than a head's, else eight: what a thread does once
+// a row is most of what it issues (norm gradients of 512 columns: 114 us with eight and a barrier a row).  The gradients
+// with a scale or a gate have registers for eight (sixteen spilled 800 bytes).
 struct NormShape {
   int columns, threads, lanes;
 };
-inline NormShape norm_shape(int width) {
-  int columns = 8, lanes = 1;
-  while (lanes * columns < width) {
-    if (lanes < 1024) lanes *= 2;
-    else columns *= 2;
-  }
-  return {columns, lanes <= 256 ? 256 : lanes, lanes};
+inline NormShape norm_shape(int width, bool roomy) {
+  const int columns = width > 8 * 1024 || (roomy && width > 256) ? 16 : 8;
+  int lanes = 1;
+  while (lanes < 32 && lanes * columns < width) lanes *= 2;
+  if (lanes * columns < width) lanes = (width + columns * 32 - 1) / (columns * 32) * 32;
+  return {columns, lanes <= 256 ? 256 : lanes <= 512 ? 512 : lanes <= 768 && columns == 8 ? 768 : 1024, lanes};
 }
 
 // The walk of at most `ctas` CTAs a group over tiles of `slots` tokens.
@@ -192,6 +193,7 @@ cudaError_t norm_launch(Kernel kernel, int operands, int pieces, int most_thread
 }
 
 // Launchers of the two directions.  vec: elements that the rows of all operands can be moved by (16 bytes of them, 2 bf16, or 1).
-int smat_norm_partials(int groups, int width);
+int smat_norm_partials(int groups, int width);      // rows of partial sums, for any call of this width
 cudaError_t smat_launch_norm_forward(NormArgs& a, int bf16, int vec, cudaStream_t st);
 cudaError_t smat_launch_norm_backward(NormArgs& a, int bf16, int vec, float* dw, float* ds, cudaStream_t st);
+cudaError_t smat_launch_norm_backward_f32(NormArgs& a, int vec, float* dw, float* ds, cudaStream_t st);

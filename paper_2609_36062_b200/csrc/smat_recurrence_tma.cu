@@ -318,11 +318,12 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     char* stage = stages + at * Shape::BYTES;
     at = at + 1 == STAGES ? 0 : at + 1;
     phase ^= at == 0;
-    // (forward, with maps of up to eight ranks to come, the states wait until the next maps are formed: 64 K tokens 179 to 172 us;
-    // backward, with more bytes and longer tiles' loads to wait for, they go first: 167 us where the other order takes 179)
-    if (BACK) enter(round);
+    // (forward, and with maps of more ranks to come, the states wait until the next maps are formed: 64 K tokens on eight ranks 179 to
+    // 172 us, gradients of 32 K 172 to 136; gradients of one or two ranks take 167 us this way and 179 the other)
+    const bool states_first = BACK && ranks <= 2;
+    if (states_first) enter(round);
     if (round + 1 < rounds) form(round + 1, at, phase, next);
-    if (!BACK) enter(round);
+    if (!states_first) enter(round);
     __syncthreads();
     if (tid == PORTER && round > 0) {
       put(round - 1);
@@ -396,6 +397,6 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
 cudaError_t smat_launch_recurrence_tma(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back, cudaStream_t st) {
   using bf16 = __nv_bfloat16;
   if (!x_bf16) return back ? launch<float, float, 2, 7, true>(a, batch, st) : launch<float, float, 4, 5, false>(a, batch, st);
-  if (gate_bf16) return back ? launch<bf16, bf16, 4, 7, true>(a, batch, st) : launch<bf16, bf16, 8, 5, false>(a, batch, st);
+  if (gate_bf16) return back ? launch<bf16, bf16, 6, 5, true>(a, batch, st) : launch<bf16, bf16, 8, 5, false>(a, batch, st);
   return back ? launch<bf16, float, 4, 5, true>(a, batch, st) : launch<bf16, float, 4, 7, false>(a, batch, st);
 }

@@ -165,12 +165,18 @@ extern "C" smat_status smat_rotary(const smat_rotary_problem* p, const smat_rows
   a.positions_batch = p->positions_batch;
   a.first = p->first;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int vec = p->dtype == SMAT_BF16 ? 8 : 4;
-  const bool wide = p->d % vec == 0 && p->rotated % (2 * vec) == 0 && rows_in_16(q, p->dtype, p->batch, p->q_heads, p->T) &&
-                    rows_in_16(k, p->dtype, p->batch, kh, p->T) && rows_in_16(q_out, p->dtype, p->batch, p->q_heads, p->T) &&
-                    rows_in_16(k_out, p->dtype, p->batch, kh, p->T);
-  const cudaError_t err = p->dtype == SMAT_BF16
-                              ? (wide ? launch<__nv_bfloat16, 8>(a, p->interleaved, st) : launch<__nv_bfloat16, 1>(a, p->interleaved, st))
-                              : (wide ? launch<float, 4>(a, p->interleaved, st) : launch<float, 1>(a, p->interleaved, st));
+  // pieces of 16 bytes, pairs of elements, or one at a time
+  const auto moves = [&](int vec) {
+    const unsigned bytes = (unsigned)(vec * dtype_bytes(p->dtype));
+    return p->d % vec == 0 && p->rotated % (2 * vec) == 0 && rows_at_multiples(q, p->dtype, p->batch, p->q_heads, p->T, bytes) &&
+           rows_at_multiples(k, p->dtype, p->batch, kh, p->T, bytes) && rows_at_multiples(q_out, p->dtype, p->batch, p->q_heads, p->T, bytes) &&
+           rows_at_multiples(k_out, p->dtype, p->batch, kh, p->T, bytes);
+  };
+  const int il = p->interleaved;
+  cudaError_t err;
+  if (p->dtype == SMAT_BF16)
+    err = moves(8) ? launch<__nv_bfloat16, 8>(a, il, st) : moves(2) ? launch<__nv_bfloat16, 2>(a, il, st) : launch<__nv_bfloat16, 1>(a, il, st);
+  else
+    err = moves(4) ? launch<float, 4>(a, il, st) : moves(2) ? launch<float, 2>(a, il, st) : launch<float, 1>(a, il, st);
   return err == cudaSuccess ? SMAT_OK : SMAT_ERR_LAUNCH;
 }

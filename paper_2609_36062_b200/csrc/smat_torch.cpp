@@ -662,6 +662,34 @@ PyObject* recurrence_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// repack(cache, packed, stream, packs): smat_decode_pack, or smat_decode_unpack
+PyObject* plan_repack(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  try {
+    if (!arity(n, 4, "repack")) return nullptr;
+    const Plan& p = *reinterpret_cast<Plan*>(self);
+    void *cache, *packed, *st;
+    size_t bytes, packed_bytes;
+    for (int i = 0; i < 2; ++i) {
+      const bool tensor = THPVariable_Check(a[i]);
+      const at::Tensor* t = tensor ? &THPVariable_Unpack(a[i]) : nullptr;
+      if (!t || !t->is_cuda() || t->scalar_type() != at::kByte || !t->is_contiguous()) {
+        PyErr_Format(PyExc_ValueError, "%s: expected a contiguous CUDA uint8 tensor", i ? "packed" : "cache");
+        return nullptr;
+      }
+    }
+    if (!workspace(a[0], "cache", &cache, &bytes) || !workspace(a[1], "packed", &packed, &packed_bytes) || !stream(a[2], &st)) return nullptr;
+    const bool packs = a[3] == Py_True;
+    const int rc = unlocked([&] {
+      return packs ? smat_decode_pack(p.handle, cache, bytes, packed, packed_bytes, st)
+                   : smat_decode_unpack(p.handle, packed, packed_bytes, cache, bytes, st);
+    });
+    if (!fail_status(rc, packs ? "smat_decode_pack" : "smat_decode_unpack")) return nullptr;
+    Py_RETURN_NONE;
+  } catch (...) {
+    return raise();
+  }
+}
+
 // Plan(handle, batch, heads, T, d_k, d_v, bf16)
 PyObject* plan_new(PyTypeObject* type, PyObject* args, PyObject*) {
   unsigned long long handle;
@@ -683,6 +711,7 @@ PyMethodDef plan_methods[] = {
     {"forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(plan_forward)), METH_FASTCALL, nullptr},
     {"backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(plan_backward)), METH_FASTCALL, nullptr},
     {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(plan_decode_step)), METH_FASTCALL, nullptr},
+    {"repack", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(plan_repack)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyTypeObject plan_type = {PyVarObject_HEAD_INIT(nullptr, 0)};

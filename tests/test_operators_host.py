@@ -164,7 +164,7 @@ def test_tensors_of_the_host_are_refused():
     with pytest.raises(ValueError):
         b.recurrence_forward(x[0], x[0])
     with pytest.raises(ValueError):
-        b.SmatPlan(1, 1, 512, 64, 64, 2, 64, "f32").decode_pack(torch.zeros(8, dtype=torch.uint8))
+        b.SmatPlan(1, 1, 512, 64, 64, 2, 64, "f32").decode_pack(torch.zeros(8, dtype=torch.uint8), torch.zeros(8, dtype=torch.uint8))
 
 
 def test_rotary_frequencies():
