@@ -138,7 +138,7 @@ cudaError_t launch(NormArgs& a, const NormShape& s, cudaStream_t st) {
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   // as many CTAs as run at once, a group's share of them each, but none without a row
   norm_walk(&a, slots, (uint32_t)(NORM_SMS * norm_ctas_an_sm(norm_resident(MODE, E), threads)) / a.groups);
-  return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 8, THREADS,
+  return norm_launch(norm_forward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 8, 0, THREADS,
                      norm_ctas_an_sm(norm_resident(MODE, E), threads),
                      dim3(a.ctas * a.groups), threads, st, a);
 }

@@ -181,11 +181,12 @@ inline int norm_ctas_an_sm(int resident, uint32_t threads) { return threads >= (
 // get as many of them: they ask for so much shared memory that no more fit.  (Where a fourth one fitted beside three, SMs that
 // drained early took four of the next launch and left others with two: the gated norm of heads took 167 us for 132.)
 template <typename Kernel>
-cudaError_t norm_launch(Kernel kernel, int operands, int pieces, int most_threads, int an_sm, dim3 grid, uint32_t threads, cudaStream_t st, const NormArgs& a) {
+cudaError_t norm_launch(Kernel kernel, int operands, int pieces, size_t least, int most_threads, int an_sm, dim3 grid, uint32_t threads, cudaStream_t st, const NormArgs& a) {
   size_t bytes = operands && norm_rings(operands, most_threads) ? (size_t)norm_depth(operands, pieces, most_threads) * operands * threads * 16 : 0;
-  const size_t no_more = (size_t)228 * 1024 / (an_sm + 1) - 1024 + 256;
+  if (bytes < least) bytes = least;
+  const size_t no_more = (size_t)228 * 1024 / (an_sm + 1) - 1024 + 256;      // (1 KB a CTA is the system's)
   if (bytes < no_more && an_sm > 2) bytes = no_more;
-  if (bytes + (pieces > 8 ? 9216 : 512) > 48 * 1024) {      // (with the sums and exchanges that a kernel has besides)
+  if (bytes + 512 > 48 * 1024) {      // (with the exchange that a kernel has besides)
     const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (err != cudaSuccess) return err;
   }

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
   pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
   if constexpr (RING) ring.landed();
   // this CTA's partial rows: the slots of a column in order
-  __shared__ float sums[THREADS == 256 ? 256 * E : 1];
+  float* sums = reinterpret_cast<float*>(rows_shared);      // (in the place of the rows, which have been read)
 #pragma unroll
   for (int which = 0; which < (SCALE ? 2 : 1); ++which) {
     float* part = which ? a.ds : a.dw;
@@ -262,7 +262,7 @@ cudaError_t launch(NormArgs& a, const NormShape& s, float* dw, float* ds, cudaSt
   a.lanes = s.lanes;
   const uint32_t threads = s.lanes <= 32 ? 256 : s.lanes, slots = threads / s.lanes;
   norm_walk(&a, slots, (uint32_t)(NORM_SMS * norm_ctas_an_sm(512, threads)) / a.groups);
-  cudaError_t err = norm_launch(norm_backward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 16,
+  cudaError_t err = norm_launch(norm_backward_kernel<T, VEC, E, THREADS, MODE>, VEC * sizeof(T) == 16 ? norm_operands(MODE) * E / VEC : 0, 16, slots > 1 ? 256 * E * sizeof(float) : 0,
                                 THREADS, norm_ctas_an_sm(512, threads), dim3(a.ctas * a.groups), threads, st, a);
   if (err != cudaSuccess || (!dw && !ds)) return err;
   const int grouped = a.weight_group ? 1 : 0;
