@@ -446,7 +446,8 @@ smat_status smat_rotary(const smat_rotary_problem* problem, const smat_rows* q, 
  *     dgate  the gradient at the gate  (NULL unless gate is given; may be gate)
  *     dweight [like weight], dscale [width]: fp32, summed over rows in a fixed order (the same from run to run); NULL: not wanted;
  *            dscale needs x.
- * workspace: DEVICE, 256-byte aligned, smat_norm_workspace_bytes(problem) bytes (only where dweight or dscale is wanted). */
+ * workspace: DEVICE, 256-byte aligned, smat_norm_workspace_bytes(problem) bytes (only where dweight or dscale is wanted); it
+ * serves one call at a time. */
 typedef enum { SMAT_ACT_SILU = 0, SMAT_ACT_SIGMOID = 1 } smat_activation;
 typedef struct {
   int batch;
@@ -473,7 +474,8 @@ smat_status smat_norm_backward(const smat_norm_problem* problem, const smat_rows
  * (NULL: not wanted) receives h_{T-1}, unrounded, and may be h0, so that T = 1 is a decoding step.  log-gates <= 0 as in
  * smat_forward_gated, in gate_dtype (that of x, or fp32).  A closed gate (log_a = -inf) forgets all of what came before, values
  * that are not finite among it: with one at the first token of every sequence, packed sequences do not see one another.
- * The state is fp32.  h may be x.
+ * The state is fp32.  h may be x.  (Kernels of long sequences wait for copies and for one another within a cluster; a wait that ran
+ * out, after two seconds, leaves NaN in what follows.)
  * Backward: from dh (and dhT, the gradient at hT, NULL: none) and the h that was kept,
  *     c_t = exp(log_a_t) (dh_t + c_{t+1}),  c_T = dhT;    dx_t = dh_t + c_{t+1},  dlog_a_t = c_t h_{t-1},  dh0 = c_0
  * dx like x (may be dh), dlog_a like log_a (may be log_a), dh0 fp32 (NULL: not wanted; may be dhT).

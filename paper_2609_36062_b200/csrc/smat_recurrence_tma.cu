@@ -387,7 +387,7 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
     uint64_t bits = reinterpret_cast<uintptr_t>(data) | (uint64_t)(s.token * bytes);
     if (batch > 1) bits |= (uint64_t)(s.batch * bytes);
     const int64_t most = (int64_t)1 << 36;
-    return (bits & 15) == 0 && s.token > 0 && s.token < most && (batch == 1 || (s.batch > 0 && s.batch < most));
+    return (bits & 15) == 0 && s.token >= a.channels && s.token < most && (batch == 1 || (s.batch > 0 && s.batch < most));
   };
   const int x = x_bf16 ? 2 : 4, g = gate_bf16 ? 2 : 4;
   return fits(a.x, a.xs, x) && fits(a.log_a, a.as, g) && fits(a.out, a.os, x) && (!back || (fits(a.h, a.hs, x) && fits(a.dlog_a, a.das, g)));

@@ -71,6 +71,10 @@ bool workspace(PyObject* o, const char* name, void** ptr, size_t* bytes) {
     return false;
   }
   const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s: expected a contiguous CUDA tensor", name);
+    return false;
+  }
   *ptr = t.data_ptr();
   *bytes = (size_t)t.numel();
   return true;
@@ -561,6 +565,9 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       ws = own.data_ptr();
     } else if (!workspace(a[12], "workspace", &ws, &bytes)) {
       return nullptr;
+    } else if (THPVariable_Unpack(a[12]).device() != H->device()) {
+      PyErr_SetString(PyExc_ValueError, "workspace: on another device than H");
+      return nullptr;
     }
     const smat_rows dy = rows_of(*dY, axes), h = rows_of(*H, axes), dh = rows_of(dH, axes);
     smat_rows g{}, dg{}, di{}, x{}, dx{};
@@ -669,14 +676,6 @@ PyObject* plan_repack(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     const Plan& p = *reinterpret_cast<Plan*>(self);
     void *cache, *packed, *st;
     size_t bytes, packed_bytes;
-    for (int i = 0; i < 2; ++i) {
-      const bool tensor = THPVariable_Check(a[i]);
-      const at::Tensor* t = tensor ? &THPVariable_Unpack(a[i]) : nullptr;
-      if (!t || !t->is_cuda() || t->scalar_type() != at::kByte || !t->is_contiguous()) {
-        PyErr_Format(PyExc_ValueError, "%s: expected a contiguous CUDA uint8 tensor", i ? "packed" : "cache");
-        return nullptr;
-      }
-    }
     if (!workspace(a[0], "cache", &cache, &bytes) || !workspace(a[1], "packed", &packed, &packed_bytes) || !stream(a[2], &st)) return nullptr;
     const bool packs = a[3] == Py_True;
     const int rc = unlocked([&] {

@@ -233,7 +233,8 @@ def test_refusals():
            lambda: f(weight=w[:32]), lambda: f(weight=w.cpu()), lambda: f(weight=torch.ones(3, 64, device=DEV)), lambda: f(residual=x[:1]),
            lambda: f(gate=x.bfloat16()), lambda: f(scale=w[:1]), lambda: f(Y=x[:1]), lambda: f(activation="tanh"),
            lambda: f(X=x[0], weight=torch.ones(4, 64, device=DEV)), lambda: k(dY=x[:1]), lambda: k(scale=w), lambda: k(dH=x.bfloat16()),
-           lambda: k(gate=x, dgate=x[:1])]
+           lambda: k(gate=x, dgate=x[:1]), lambda: k(workspace=torch.zeros(1 << 20, dtype=torch.uint8)),
+           lambda: k(workspace=torch.zeros(1 << 22, dtype=torch.uint8, device=DEV)[::2])]
     for i, call in enumerate(bad):
         with pytest.raises(ValueError):
             call()

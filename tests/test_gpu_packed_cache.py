@@ -261,9 +261,13 @@ def test_captured_steps_and_refusals():
     want = plan.decode_step_packed(*row, n, two)
     torch.cuda.synchronize()
     assert torch.equal(o, want) and torch.equal(one, two) and torch.equal(Cache(plan, spare, True).S, Cache(plan, one, True).S)
-    for bad in (one[:1024], one.view(torch.int8), one.cpu()):
+    for bad in (one[:1024], one.cpu(), one.repeat(2)[::2]):
         with pytest.raises((b.SmatError, ValueError)):
             plan.decode_unpack(bad)
+        with pytest.raises((b.SmatError, ValueError)):
+            plan.decode_step_packed(*row, n, bad)
+        with pytest.raises((b.SmatError, ValueError)):
+            plan.decode_begin_packed(dev["k"], dev["v"], bad)
     with pytest.raises(b.SmatError):
         plan.decode_step_packed(*row, n, one[:1024])
     with pytest.raises(b.SmatError):

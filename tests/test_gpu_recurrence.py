@@ -174,6 +174,19 @@ def test_strides_and_outputs_in_place():
     assert bool((out[..., C:] == 5).all())
 
 
+@pytest.mark.parametrize("types", TYPES)
+def test_broadcast_and_overlapping_rows(types):
+    """Inputs that repeat (stride 0 over sequences, over tokens) or overlap: no tensor map, an address each."""
+    x, log_a, h0, dhT, g = inputs(3, 150, 64, types, 21)
+    one, gate = x[:1].expand(3, 150, 64), log_a[:, :1].expand(3, 150, 64)
+    H, _ = check_forward(one, gate, h0)
+    check_backward(gate, one, H, h0, dhT)
+    wide = torch.randn(3, 150 * 32 + 64, generator=g, device=DEV).to(types[0])
+    slid = wide.as_strided((3, 150, 64), (wide.shape[1], 32, 1))
+    H, _ = check_forward(slid, log_a, h0)
+    check_backward(log_a, slid, slid, h0, dhT)
+
+
 def test_gradients_against_differences():
     x, log_a, h0, dhT, g = inputs(1, 70, 5, TYPES[2], 9)
     dH = torch.randn(1, 70, 5, generator=g, device=DEV)
