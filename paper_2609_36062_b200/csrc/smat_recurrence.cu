@@ -64,20 +64,35 @@ struct Share {
   }
 };
 
+// One channel of a share's token l, from the state before it.  Backward the output v_t = x_t + c_{t+1} is carried instead of the state
+// c_t = a_t v_t, so that a token is one fused product and sum either way, and the values behind a closed gate are the same, bit for
+// bit, whatever came before it.
+template <bool CLOSED, bool BACK, int VEC, int STEPS>
+__device__ __forceinline__ void advance(const float (&gate)[STEPS][VEC], int l, int i, float x, float& v, float& state) {
+  const float a = gate[l][i];
+  if (BACK) {
+    const float before = l ? gate[l ? l - 1 : 0][i] : 1.f;
+    if (l == 0) v = x + state;
+    else v = CLOSED ? rec_step(before, v, x) : fmaf(before, v, x);
+    state = CLOSED && a == 0.f ? 0.f : a * v;
+  } else {
+    v = state = CLOSED ? rec_step(a, state, x) : fmaf(a, state, x);
+  }
+}
+
 // The map (A, H) of a share's tokens.
 template <bool CLOSED, typename TX, typename TA, int VEC, int STEPS, bool BACK>
 __device__ __forceinline__ void map_of(const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC], float (&A)[VEC],
                                        float (&H)[VEC]) {
+  float v[VEC];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) { A[i] = 1.f; H[i] = 0.f; }
+  for (int i = 0; i < VEC; ++i) { A[i] = 1.f; H[i] = v[i] = 0.f; }
 #pragma unroll
   for (int l = 0; l < STEPS; ++l) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      const float a = gate[l][i], x = in.x[l].get(i);
-      A[i] *= a;
-      if (CLOSED && a == 0.f) H[i] = BACK ? 0.f : x;
-      else H[i] = BACK ? a * (H[i] + x) : fmaf(a, H[i], x);
+      A[i] *= gate[l][i];
+      advance<CLOSED, BACK>(gate, l, i, in.x[l].get(i), v[i], H[i]);
     }
   }
 }
@@ -87,23 +102,20 @@ __device__ __forceinline__ void map_of(const Share<TX, TA, VEC, STEPS, BACK>& in
 template <bool CLOSED, typename TX, typename TA, int VEC, int STEPS, bool BACK, typename OFF>
 __device__ __forceinline__ float apply(const Share<TX, TA, VEC, STEPS, BACK>& in, const float (&gate)[STEPS][VEC], float (&state)[VEC],
                                        const Place<TX, OFF>& op, const Place<TA, OFF>& dap, const float* h0, int count, int64_t left) {
-  float zeros = 0.f;
+  float zeros = 0.f, v[VEC], d[VEC];
   const bool last = BACK && left <= STEPS;
 #pragma unroll
+  for (int i = 0; i < VEC; ++i) v[i] = 0.f;
+#pragma unroll
   for (int l = 0; l < STEPS; ++l) {
-    float v[VEC], d[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      const float a = gate[l][i], x = in.x[l].get(i);
+      advance<CLOSED, BACK>(gate, l, i, in.x[l].get(i), v[i], state[i]);
       if (BACK) {
-        v[i] = x + state[i];                                           // dx
-        state[i] = CLOSED && a == 0.f ? 0.f : a * v[i];                // c
         float before = in.h[BACK ? l : 0].get(i);
         if (last && l + 1 == left && h0) before = h0[i];
-        d[i] = CLOSED && a == 0.f ? 0.f : state[i] * before;
+        d[i] = CLOSED && gate[l][i] == 0.f ? 0.f : state[i] * before;
         zeros = fmaf(d[i], 0.f, zeros);
-      } else {
-        v[i] = state[i] = CLOSED ? rec_step(a, state[i], x) : fmaf(a, state[i], x);
       }
     }
     if (l < count) {

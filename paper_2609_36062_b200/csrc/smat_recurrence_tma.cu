@@ -12,7 +12,9 @@
 // ahead, so that a round hides their way.  What sends the map of round n + 1 comes after a barrier behind all reads of those of
 // round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
 //
-// It is the number of instructions that bounds it: 64 K tokens of 2048 bf16 channels took MEASURED
+// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 171 us where their
+// bytes take 122 (0.72 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
+// round ahead and pairs of channels the first took 233 us.
 #include <type_traits>
 
 #include "smat_recurrence.cuh"
@@ -195,6 +197,28 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     float2 gate[STEPS];
     RowVec<TX, VEC> x[STEPS];
   };
+  // The states behind a thread's tokens, from `state` on: put(l, what leaves as the output, the state behind the token) for each.
+  // Backward the output v_t = x_t + c_{t+1} is carried instead of the state c_t = a_t v_t, so that a token is one fused product and sum
+  // either way, and the values behind a closed gate are the same, bit for bit, whatever came before it.
+  const auto states = [](const Tokens& k, auto closed, float2 state, auto put) {
+    constexpr bool CLOSED = decltype(closed)::value;
+    [[maybe_unused]] float2 v = state;
+#pragma unroll
+    for (int l = 0; l < STEPS; ++l) {
+      const float2 x = pair(k.x[l]);
+      if constexpr (BACK) {
+        if (l == 0) v = __fadd2_rn(x, state);
+        else v = CLOSED ? closed_step(k.gate[l - 1], v, x) : __ffma2_rn(k.gate[l - 1], v, x);
+        state = __fmul2_rn(k.gate[l], v);
+        if (CLOSED) state = unless_closed(k.gate[l], state);
+        put(l, v, state);
+      } else {
+        state = CLOSED ? closed_step(k.gate[l], state, x) : __ffma2_rn(k.gate[l], state, x);
+        put(l, state, state);
+      }
+    }
+    return state;
+  };
   const auto form = [&](int round, int stage, uint32_t phase, Tokens& k) {
     float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
     if (round < own_rounds) {
@@ -209,16 +233,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       }
       open_gates(a, k.gate);
 #pragma unroll
-      for (int l = 0; l < STEPS; ++l) {
-        A = __fmul2_rn(A, k.gate[l]);
-        H = BACK ? __fmul2_rn(k.gate[l], __fadd2_rn(H, pair(k.x[l]))) : __ffma2_rn(k.gate[l], H, pair(k.x[l]));
-      }
-      if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) {
-        H = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int l = 0; l < STEPS; ++l)
-          H = BACK ? unless_closed(k.gate[l], __fmul2_rn(k.gate[l], __fadd2_rn(H, pair(k.x[l])))) : closed_step(k.gate[l], H, pair(k.x[l]));
-      }
+      for (int l = 0; l < STEPS; ++l) A = __fmul2_rn(A, k.gate[l]);
+      const auto nothing = [](int, float2, float2) {};
+      H = states(k, std::false_type(), make_float2(0.f, 0.f), nothing);
+      if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) H = states(k, std::true_type(), make_float2(0.f, 0.f), nothing);
       if (lost) H = make_float2(NAN, NAN);
     }
     *reinterpret_cast<float4*>(&warp_map[round & 1][warp][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
@@ -280,32 +298,24 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     const float2 from = *reinterpret_cast<const float2*>(&entering[round & 1][warp][lane * VEC]);
     const bool first = BACK && token_of(round) == 0 && warp == REC_WARPS - 1;      // token 0 is this thread's last
     const auto go = [&](auto closed) {
-      constexpr bool CLOSED = decltype(closed)::value;
+      [[maybe_unused]] constexpr bool CLOSED = decltype(closed)::value;
       const float2 none = make_float2(0.f, 0.f);
-      float2 s = from, zeros = none;
-#pragma unroll
-      for (int l = 0; l < STEPS; ++l) {
-        const float2 a = k.gate[l];
+      float2 zeros = none;
+      const float2 behind = states(k, closed, from, [&](int l, float2 out, float2 state) {
+        store_piece<TX>(out, xs + l * WAY * (int)sizeof(TX));
         if constexpr (BACK) {
-          const float2 v = __fadd2_rn(pair(k.x[l]), s);                // dx
-          s = __fmul2_rn(a, v);                                        // c
-          if (CLOSED) s = unless_closed(a, s);
           float2 before = pair(load_piece<TX>(hs + l * WAY * (int)sizeof(TX)));
           if (l == STEPS - 1 && first && h0) {
             const int c = lane * VEC;
             before = make_float2(c0 + c < channels ? h0[row + c] : 0.f, c0 + c + 1 < channels ? h0[row + c + 1] : 0.f);
           }
-          float2 d = __fmul2_rn(s, before);
-          if (CLOSED) d = unless_closed(a, d);
+          float2 d = __fmul2_rn(state, before);
+          if (CLOSED) d = unless_closed(k.gate[l], d);
           else zeros = __ffma2_rn(d, none, zeros);
-          store_piece<TX>(v, xs + l * WAY * (int)sizeof(TX));
           store_piece<TA>(d, as + l * WAY * (int)sizeof(TA));
-        } else {
-          s = CLOSED ? closed_step(a, s, pair(k.x[l])) : __ffma2_rn(a, s, pair(k.x[l]));
-          store_piece<TX>(s, xs + l * WAY * (int)sizeof(TX));
         }
-      }
-      zeros = __ffma2_rn(s, none, zeros);
+      });
+      zeros = __ffma2_rn(behind, none, zeros);
       return zeros.x + zeros.y;
     };
     if (rec_not_finite(go(std::false_type()))) go(std::true_type());
@@ -393,7 +403,8 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
   return fits(a.x, a.xs, x) && fits(a.log_a, a.as, g) && fits(a.out, a.os, x) && (!back || (fits(a.h, a.hs, x) && fits(a.dlog_a, a.das, g)));
 }
 
-// Stages and tokens of a tile: two CTAs an SM, with two tiles or more on their way.
+// Stages and tokens of a tile: two CTAs an SM, with two tiles or more on their way.  (One CTA of tiles three times as long issues half
+// the instructions a token, but eight warps an SM do not hide their latency: 64 K tokens 260 us.)
 cudaError_t smat_launch_recurrence_tma(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back, cudaStream_t st) {
   using bf16 = __nv_bfloat16;
   if (!x_bf16) return back ? launch<float, float, 2, 7, true>(a, batch, st) : launch<float, float, 4, 5, false>(a, batch, st);
