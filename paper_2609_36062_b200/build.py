@@ -98,7 +98,7 @@ def _build_extension(versions: str, verbose: bool) -> None:
     compile_ = [CXX, "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     compile_ += [f"-I{d}" for d in inc] + ["-c", EXT_SRC, "-o", obj]
     link = [CXX, "-shared", "-o", EXT, obj, f"-L{os.path.join(root, 'lib')}", "-ltorch_python", "-ltorch", "-ltorch_cpu",
-            "-lc10", "-lc10_cuda", f"-L{HERE}", "-l:libsmat.so", "-Wl,-rpath,$ORIGIN"]
+            "-ltorch_cuda", "-lc10", "-lc10_cuda", f"-L{HERE}", "-l:libsmat.so", "-Wl,-rpath,$ORIGIN"]
     _run([compile_], "compiling _smat_torch.so", verbose)
     _run([link], "linking _smat_torch.so", verbose)
     with open(EXT_VERSIONS, "w") as f:
