@@ -1,9 +1,9 @@
 // What the norm's two directions share: arguments, the layout of a row over lanes, sums over a row, the gate's function.
 //
-// A row of `width` columns belongs to `lanes` lanes (a power of two), each with E columns of it in registers, VEC at a time: columns
-// (n * lanes + lane) * VEC for n < E / VEC.  Rows of a head are held by part of a warp or a warp and meet by shuffles; rows of a
+// A row of `width` columns belongs to `lanes` lanes (part of a warp: a power of two, or whole warps), each with E columns of it in
+// registers, VEC at a time: columns (n * lanes + lane) * VEC for n < E / VEC.  Rows of a head are held by part of a warp or a warp and meet by shuffles; rows of a
 // model by a CTA.  A CTA's rows all belong to one group, so that its weights stay in registers while it walks over the rows;
-// the next row is on its way while one is summed.  Groups are the fastest part of the CTA's number: the CTAs that run together
+// the next rows are on their way while one is summed.  Groups are the fastest part of the CTA's number: the CTAs that run together
 // cover the same tokens of all groups, whichever of the two layouts ([b, h, T, d] or [b, T, h, d]) a tensor has.
 #pragma once
 #include <cuda_runtime.h>
@@ -68,7 +68,7 @@ __device__ __forceinline__ void norm_move(T*& p, const NormOperand& o, bool wrap
 }
 
 // What a kernel is compiled for: rows alone, with the residual stream (forward) or the branch's scale (backward), behind a block with
-// one of the gates, or anything, decided by the operands that are given (rows that move by one or two elements only have this one).
+// one of the gates, or anything, decided by the operands that are given.
 // A kernel that asks at run time issues twice the instructions of one that does not, and it is instructions that bound the gated
 // norms of heads.
 enum NormMode { NORM_ROWS, NORM_STREAM, NORM_SILU, NORM_SIGMOID, NORM_ANY };

@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1) norm_backward
     if constexpr (RING) load();      // (into the places that have just been read)
     float sum[2] = {squares.x + squares.y, products.x + products.y};
     norm_row_sum(sum, a.lanes, turn, exchange);
-    const float r = rsqrtf(fmaf(sum[0], a.inv_width, a.eps));
+    const float r = here ? rsqrtf(fmaf(sum[0], a.inv_width, a.eps)) : 0.f;      // (a slot without a row adds nothing, at eps = 0 either)
     const float2 rs = norm_both(r), mean = norm_both(-r * (sum[1] * r * a.inv_width));      // -r mean(dn n)
     float2 dh[E / 2];
 #pragma unroll

@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
                                                                         float* end, int T, int channels) {
   using Shape = Tile<TX, TA, STEPS, BACK>;
   static_assert(STAGES >= 4, "a round's tile is asked for two rounds before its map is formed, one round ahead");
-  static_assert(REC_THREADS == 4 * COLS && 32 * VEC == COLS, "half of the threads join the states of a channel, half send its map");
+  static_assert(REC_THREADS == 4 * COLS && 32 * VEC == COLS, "one thread joins the states of a channel, another sends its map");
   extern __shared__ __align__(128) char stages[];
   __shared__ __align__(16) float2 warp_map[2][REC_WARPS][COLS];      // (A, H) of a warp's tokens, of this round and of the next
   __shared__ __align__(16) float entering[2][REC_WARPS][COLS];       // the state that enters a warp's tokens
@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   const cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int channel = tid % COLS, half = tid / COLS & 1;      // whose states (the first 128 threads) or maps this thread joins
-  const bool joins = tid < 2 * COLS;
+  const int channel = tid % COLS;      // whose states (two warps) or maps (two others) this thread joins
+  const bool joins = tid < COLS, sends = tid / COLS == 2;
   const int b = blockIdx.z, c0 = blockIdx.y * COLS;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) tc::mbar_init(&full[i], 1);
@@ -241,16 +241,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     }
     *reinterpret_cast<float4*>(&warp_map[round & 1][warp][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
   };
-  // The second 128 threads send this CTA's map of a round to all ranks, every other one each.
-  uint32_t to[REC_MAX_CLUSTER / 2], bar_in[REC_MAX_CLUSTER / 2];
-#pragma unroll
-  for (int i = 0; i < REC_MAX_CLUSTER / 2; ++i) {
-    const int r = 2 * i + half < ranks ? 2 * i + half : rank;
-    to[i] = in_rank(&tile_map[0][rank][channel], r);
-    bar_in[i] = in_rank(&maps_in[0], r);
-  }
+  // This CTA's map of a round to all ranks.  (It is what all threads issue together that counts: with the maps and states of a channel
+  // joined by two threads each, or by four in all warps alike, 64 K tokens took 171 and 188 us.)
   const auto publish = [&](int round) {
-    if (joins || ranks == 1) return;
+    if (!sends || ranks == 1) return;
     const int turn = round & 1;
     float2 m = warp_map[turn][0][channel];
 #pragma unroll
@@ -258,12 +252,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       const float2 n = warp_map[turn][w][channel];
       m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
     }
-    if (tid == PORTER) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
-#pragma unroll
-    for (int i = 0; i < REC_MAX_CLUSTER / 2; ++i)
-      if (2 * i + half < ranks) send(to[i] + turn * (uint32_t)sizeof(tile_map[0]), bar_in[i] + turn * 8u, m);
+    if (channel == 0) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
+    for (int r = 0; r < ranks; ++r) send(in_rank(&tile_map[turn][rank][channel], r), in_rank(&maps_in[turn], r), m);
   };
-  // The first 128 form the states that enter the warps' tokens, four each; the maps of a round have been on their way for a round.
+  // The states that enter the warps' tokens; the maps of a round have been on their way for a round.
   const auto enter = [&](int round) {
     if (!joins) return;
     const int turn = round & 1;
@@ -283,7 +275,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     }
 #pragma unroll
     for (int w = 0; w < REC_WARPS; ++w) {
-      if (w / (REC_WARPS / 2) == half) entering[turn][w][channel] = state;
+      entering[turn][w][channel] = state;
       const float2 m = warp_map[turn][w][channel];
       state = rec_step(m.x, state, m.y);
     }

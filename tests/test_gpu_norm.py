@@ -192,6 +192,19 @@ def test_rows_of_zeros_and_rows_that_are_not_finite():
     near(dh[:, 1], torch.full_like(dh[:, 1], EPS ** -0.5).double(), ROW * EPS ** -0.5, "dh of zeros")
 
 
+@pytest.mark.parametrize("width", [64, 128, 130, 1000, 2048])
+def test_without_epsilon(width):
+    """eps = 0 with fewer rows than a CTA has places for: the empty ones leave the sums over rows alone."""
+    g = generator(11)
+    x, dy, dh_in = (torch.randn(1, 3, width, generator=g, device=DEV) for _ in range(3))
+    w, scale = (torch.randn(width, generator=g, device=DEV) for _ in range(2))
+    near(b.norm_forward(x, w, eps=0.0), forward64(x, w, eps=0.0)[0], ROW * forward64(x, w, eps=0.0)[0].abs(), "y")
+    dH, dX, dW, dS, _ = b.norm_backward(dy, x, w, eps=0.0, dH=dh_in, X=x, scale=scale)
+    n = x.double() / torch.sqrt(x.double().square().mean(-1, keepdim=True))
+    near(dW, (dy.double() * n).sum((0, 1)), SUMS * (dy.double() * n).abs().sum((0, 1)), "dw")
+    assert bool(torch.isfinite(dH).all()) and bool(torch.isfinite(dX).all()) and bool(torch.isfinite(dS).all())
+
+
 def test_gradients_against_differences():
     """d/ds of <dy, y(h + s e)> and the like by central differences of the 64-bit formula (error s^2: 1e-6)."""
     g = generator(7)
