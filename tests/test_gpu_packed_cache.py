@@ -45,11 +45,12 @@ class Cache:
 
 
 def codes_of(table):
-    """The documented rule, in 64 bits: m = 127 / max cut to eight significant bits."""
+    """The documented rule: m = 127 / max in fp32 (a quotient next to a number of eight bits may be rounded to it), cut to eight
+    significant bits; the rest in 64 bits."""
     top = table.double().abs().amax(-1)
-    m = 127.0 / top
+    m = (127.0 / top.float()).clamp(max=2.0 ** 126).double()
     unit = torch.exp2(torch.floor(torch.log2(m)) - 7)
-    m = torch.where(top > 0, (torch.floor(m / unit) * unit).clamp(max=2.0 ** 126), torch.zeros_like(top))
+    m = torch.where(top > 0, torch.floor(m / unit) * unit, torch.zeros_like(top))
     return torch.round(table.double() * m[..., None]), torch.where(m > 0, 1 / m, torch.zeros_like(m))
 
 
