@@ -9,7 +9,8 @@
 // memory (the CTA), and the thread goes over its tokens again from the state that enters them.  Every input is read once,
 // and the next tile's loads are in flight meanwhile.  Where there are too few channels and sequences to fill the GPU, the CTAs of
 // a cluster take tiles in turn and hand their tile's map to one another through distributed shared memory: one cluster barrier a
-// round, no flags in global memory, and sums in an order that is the same from run to run.
+// round, no flags in global memory, and sums in an order that is the same from run to run.  Where sequences are many and short, a
+// thread takes its channels of a whole sequence instead (rec_sequential).
 //
 // Bound by HBM.  A closed gate (a = 0) drops what came before it, also where that is not finite.
 #include <type_traits>
@@ -166,32 +167,43 @@ __device__ __forceinline__ void gates_of(const Share<TX, TA, VEC, STEPS, BACK>& 
     for (int i = 0; i < VEC; ++i) gate[l][i] = expf(in.a[l].get(i));
 }
 
-// Short sequences: a thread takes VEC channels of a sequence from the first token to the last.
-template <typename TX, typename TA, int VEC, bool BACK>
-__global__ void __launch_bounds__(REC_THREADS) recurrence_short_kernel(const RecArgs p, uint32_t pieces) {
-  constexpr int STEPS = 2;
+// Sequences that are short for their number: a thread takes VEC channels of a sequence from the first token to the last, STEPS of them
+// while the next STEPS are on their way.  No maps, nothing to join.
+constexpr int SEQ_THREADS = 128;
+template <typename TX, typename TA, int VEC, int STEPS, bool BACK>
+__global__ void __launch_bounds__(SEQ_THREADS) recurrence_sequential_kernel(const RecArgs p, uint32_t pieces) {
   pdl_trigger();
-  const uint32_t n = blockIdx.x * REC_THREADS + threadIdx.x, b = blockIdx.y;
+  const uint32_t n = blockIdx.x * SEQ_THREADS + threadIdx.x, b = blockIdx.y;
   pdl_wait();
   if (n >= pieces) return;
   const int c = (int)n * VEC;
   const int64_t row = (int64_t)b * p.channels + c;
-  const auto place = [&](auto* data, const RowStride& at, int64_t s, int before) {
+  const auto place = [&](auto* data, const RowStride& at, int before) {
     using P = Place<std::remove_const_t<std::remove_pointer_t<decltype(data)>>, uint64_t>;
-    return P{data + b * at.batch + (BACK ? p.T - 1 - s - before : s) * at.token + c, BACK ? -at.token : at.token, 0};
+    return P{data + b * at.batch + (BACK ? p.T - 1 - before : 0) * at.token + c, BACK ? -at.token : at.token, 0};
   };
+  auto xp = place(static_cast<const TX*>(p.x), p.xs, 0), hp = place(static_cast<const TX*>(p.h), p.hs, 1);
+  auto ap = place(static_cast<const TA*>(p.log_a), p.as, 0);
+  auto op = place(static_cast<const TX*>(p.out), p.os, 0);
+  auto dap = place(static_cast<const TA*>(p.dlog_a), p.das, 0);
+  const auto move = [](auto& at) { at.base += STEPS * at.token; };
+  const auto count_at = [&](int64_t left) { return left < 0 ? 0 : (int)(left < STEPS ? left : STEPS); };
   float state[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) state[i] = p.begin ? p.begin[row + i] : 0.f;
-  for (int64_t s = 0; s < p.T; s += STEPS) {
-    const int count = (int)(p.T - s < STEPS ? p.T - s : STEPS);
-    Share<TX, TA, VEC, STEPS, BACK> in;
-    in.load(place(static_cast<const TX*>(p.x), p.xs, s, 0), place(static_cast<const TA*>(p.log_a), p.as, s, 0),
-            place(static_cast<const TX*>(p.h), p.hs, s, 1), count, p.T - s);
+  Share<TX, TA, VEC, STEPS, BACK> next;
+  next.load(xp, ap, hp, count_at(p.T), p.T);
+  for (int64_t left = p.T; left > 0; left -= STEPS) {
+    const Share<TX, TA, VEC, STEPS, BACK> in = next;
+    move(xp);
+    move(ap);
+    if (BACK) move(hp);
+    if (left > STEPS) next.load(xp, ap, hp, count_at(left - STEPS), left - STEPS);
     float gate[STEPS][VEC];
     gates_of(in, gate);
-    apply(in, gate, state, place(static_cast<const TX*>(p.out), p.os, s, 0), place(static_cast<const TA*>(p.dlog_a), p.das, s, 0),
-          p.h0 ? p.h0 + row : nullptr, count, p.T - s);
+    apply(in, gate, state, op, dap, p.h0 ? p.h0 + row : nullptr, count_at(left), left);
+    move(op);
+    if (BACK) move(dap);
   }
   if (p.end) {
 #pragma unroll
@@ -316,15 +328,20 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
 }
 
 constexpr int64_t REC_NEAR = (int64_t)1 << 24;   // elements between two of a tile's 128 tokens, where 32 bits hold a tile
-constexpr int64_t REC_SHORT = 8;          // tokens up to which a thread takes a sequence by itself
+
+// Whether a thread takes a sequence by itself.  Its time grows with T by itself, that of tiles with the waves of CTAs (a CTA takes 64
+// channels of a sequence, REC_CTAS run at once).  2048 channels of bf16, tiles against threads, in us, forward and backward:
+//   1 sequence   (1 wave)     8 tokens  2.5, 3.1  1.7, 2.2      64 tokens  2.6, 2.7  5.2, 8.8
+//   32           (4 waves)   32 tokens  8.6, 9.2  4.5, 6.9     128 tokens   13, 18    14, 33
+//   512         (56 waves)   64 tokens  151, 207   66, 115     256 tokens  325, 448  256, 456
+bool rec_sequential(const RecArgs& a, int batch, bool back) {
+  const int64_t columns = (a.channels + 63) / 64, waves = (columns * batch + REC_CTAS - 1) / REC_CTAS;
+  const int64_t most = (back ? 8 : 16) * waves, cap = back ? 128 : 256;
+  return a.T <= (most < cap ? most : cap);
+}
 
 template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK, typename OFF>
 cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
-  if (a.T <= REC_SHORT) {
-    const uint32_t pieces = (uint32_t)((a.channels + VEC - 1) / VEC);
-    return smat_launch_pdl(recurrence_short_kernel<TX, TA, VEC, BACK>, dim3((pieces + REC_THREADS - 1) / REC_THREADS, (unsigned)batch),
-                           REC_THREADS, 0, st, a, pieces);
-  }
   constexpr int COLS = LANES * VEC, TILE = REC_THREADS / LANES * STEPS;
   const int64_t columns = (a.channels + COLS - 1) / COLS, tiles = (a.T + TILE - 1) / TILE;
   const unsigned ranks = rec_ranks(columns, batch, tiles);
@@ -332,16 +349,32 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
                                  REC_THREADS, 0, ranks, st, a);
 }
 
+template <typename TX, typename TA, int VEC, bool BACK>
+cudaError_t launch_sequential(const RecArgs& a, int batch, cudaStream_t st) {
+  constexpr int STEPS = BACK || sizeof(TX) + sizeof(TA) > 4 ? 4 : 8;      // as many as registers hold twice
+  const uint32_t pieces = (uint32_t)((a.channels + VEC - 1) / VEC);
+  const dim3 grid((pieces + SEQ_THREADS - 1) / SEQ_THREADS, (unsigned)batch);
+  // Few tokens: with fewer registers more threads run at once (512 sequences of 4 tokens 4.5 us, with STEPS 8.2).
+  if (a.T <= 4) return smat_launch_pdl(recurrence_sequential_kernel<TX, TA, VEC, 2, BACK>, grid, SEQ_THREADS, 0, st, a, pieces);
+  return smat_launch_pdl(recurrence_sequential_kernel<TX, TA, VEC, STEPS, BACK>, grid, SEQ_THREADS, 0, st, a, pieces);
+}
+
 template <bool BACK>
 cudaError_t dispatch(const RecArgs& a, const smat_recurrence_problem* p, bool wide, cudaStream_t st) {
   const int x_bf16 = p->dtype == SMAT_BF16, gate_bf16 = p->gate_dtype == SMAT_BF16;
-  if (a.T > REC_SHORT && smat_recurrence_tma_supported(a, p->batch, x_bf16, gate_bf16, BACK))
+  using bf16 = __nv_bfloat16;
+  if (rec_sequential(a, p->batch, BACK)) {
+    if (p->dtype == SMAT_F32)
+      return wide ? launch_sequential<float, float, 4, BACK>(a, p->batch, st) : launch_sequential<float, float, 1, BACK>(a, p->batch, st);
+    if (gate_bf16) return wide ? launch_sequential<bf16, bf16, 4, BACK>(a, p->batch, st) : launch_sequential<bf16, bf16, 1, BACK>(a, p->batch, st);
+    return wide ? launch_sequential<bf16, float, 4, BACK>(a, p->batch, st) : launch_sequential<bf16, float, 1, BACK>(a, p->batch, st);
+  }
+  if (smat_recurrence_tma_supported(a, p->batch, x_bf16, gate_bf16, BACK))
     return smat_launch_recurrence_tma(a, p->batch, x_bf16, gate_bf16, BACK, st);
   constexpr int S = BACK ? 4 : 8;
-  using bf16 = __nv_bfloat16;
   if (p->dtype == SMAT_F32)
     return wide ? launch<float, float, 4, 16, 4, BACK, uint32_t>(a, p->batch, st) : launch<float, float, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
-  if (p->gate_dtype == SMAT_BF16)
+  if (gate_bf16)
     return wide ? launch<bf16, bf16, 4, 16, S, BACK, uint32_t>(a, p->batch, st) : launch<bf16, bf16, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
   return wide ? launch<bf16, float, 4, 16, 4, BACK, uint32_t>(a, p->batch, st) : launch<bf16, float, 1, 32, S, BACK, uint64_t>(a, p->batch, st);
 }

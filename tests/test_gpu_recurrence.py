@@ -175,6 +175,43 @@ def test_strides_and_outputs_in_place():
 
 
 @pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("B,T,C", [(1, 15, 136), (1, 17, 2048), (300, 32, 132), (300, 33, 132), (300, 63, 131), (300, 65, 132), (2000, 20, 65),
+                                   (1200, 104, 132), (1200, 105, 132), (1200, 207, 132), (1200, 209, 132)])
+def test_many_sequences(B, T, C, types):
+    """A thread a sequence, and lengths at which tiles take over, of either direction."""
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, B + T)
+    H, _ = check_forward(x, log_a, h0)
+    check_forward(x, log_a)
+    check_backward(log_a, H, torch.randn(B, T, C, generator=g, device=DEV).to(types[0]), h0, dhT)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("C", [64, 63])
+def test_closed_gates_of_many_sequences(C, types):
+    B, T = 700, 21
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, 12)
+    log_a[::2, 9] = log_a[::3, 0] = log_a[::5, 20] = -math.inf
+    H, hT = check_forward(x, log_a, h0)
+    dH = torch.randn(B, T, C, generator=g, device=DEV).to(types[0])
+    check_backward(log_a, H, dH, h0, dhT)
+    bad, hbad = x.clone(), H.clone()
+    bad[::2, 3:9] = math.nan
+    hbad[::2, 8] = math.inf
+    other, last = b.recurrence_forward(bad, log_a, h0=h0)
+    assert torch.equal(other[:, 9:], H[:, 9:]) and torch.equal(last, hT) and bool(torch.isnan(other[::2, 3:9]).all())
+    got, want = (b.recurrence_backward(log_a, h, dH, h0=h0, dhT=dhT) for h in (hbad, H))
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    # outputs in the place of inputs, rows of [T, batch, channels]
+    x, log_a = (v.transpose(0, 1).contiguous().transpose(0, 1) for v in (x, log_a))
+    state = h0.clone()
+    again, _ = b.recurrence_forward(x, log_a, h0=state, H=x, hT=state)
+    assert torch.equal(again, H) and torch.equal(state, hT)
+    end = dhT.clone()
+    got = b.recurrence_backward(log_a, again, dH, h0=h0, dhT=end, dX=dH, dlog_a=log_a, dh0=end)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("types", TYPES)
 def test_broadcast_and_overlapping_rows(types):
     """Inputs that repeat (stride 0 over sequences, over tokens) or overlap: no tensor map, an address each."""
     x, log_a, h0, dhT, g = inputs(3, 150, 64, types, 21)
