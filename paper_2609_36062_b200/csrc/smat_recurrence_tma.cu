@@ -1,8 +1,8 @@
 // The recurrence of long sequences whose tiles move by TMA (see smat_recurrence.cu for how tiles, warps and threads are joined).
 //
-// A tile is 64 channels of 8 * STEPS tokens of every operand, in one stage of a ring in shared memory; outputs take the place of
-// the inputs there and leave by TMA too.  A warp has STEPS tokens of it, a thread two channels of these: it forms their map, and
-// goes over them again from the state that enters them.  So loads and stores cost a thread one instruction of a fixed offset a
+// A tile is COLS channels of GROUPS * STEPS tokens of every operand, in one stage of a ring in shared memory; outputs take the place of
+// the inputs there and leave by TMA too.  A group of COLS / 2 threads has STEPS tokens of it, a thread two channels of these: it forms
+// their map, and goes over them again from the state that enters them.  So loads and stores cost a thread one instruction of a fixed offset a
 // token, where their addresses had taken a third of all it issued, and the next tiles are on their way without registers.
 // Tokens behind the end, and channels beyond the last, are read as zeros: x = 0 and log_a = 0 leave the state as it is.  A
 // backward pass goes over the same tiles from the last to the first, and reads h one token before dh.
@@ -12,8 +12,8 @@
 // ahead, so that a round hides their way.  What sends the map of round n + 1 comes after a barrier behind all reads of those of
 // round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
 //
-// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 171 us where their
-// bytes take 122 (0.72 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
+// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 161 us where their
+// bytes take 122 (0.76 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
 // round ahead and pairs of channels the first took 233 us.
 #include <type_traits>
 
@@ -24,13 +24,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int COLS = 64, VEC = 2;
+constexpr int VEC = 2;
 constexpr int PORTER = REC_THREADS - 32;      // the thread that issues copies
 constexpr long long WAIT_LIMIT = 4000000000LL;   // SM clock cycles before a wait gives up
 
-template <typename TX, typename TA, int STEPS, bool BACK>
+template <typename TX, typename TA, int COLS, int STEPS, bool BACK>
 struct Tile {
-  static constexpr int TOKENS = REC_WARPS * STEPS;
+  static constexpr int GROUPS = REC_THREADS * VEC / COLS, TOKENS = GROUPS * STEPS;
   static constexpr uint32_t X = TOKENS * COLS * sizeof(TX), A = TOKENS * COLS * sizeof(TA);
   static constexpr uint32_t BYTES = X + A + (BACK ? X : 0);
   static constexpr uint32_t A_AT = X, H_AT = X + A;
@@ -133,22 +133,23 @@ struct Maps {
   CUtensorMap x, log_a, h, out, dlog_a;
 };
 
-template <typename TX, typename TA, int STEPS, int STAGES, bool BACK>
+template <typename TX, typename TA, int COLS, int STEPS, int STAGES, bool BACK>
 __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __grid_constant__ Maps maps, const float* begin, const float* h0,
                                                                         float* end, int T, int channels) {
-  using Shape = Tile<TX, TA, STEPS, BACK>;
+  using Shape = Tile<TX, TA, COLS, STEPS, BACK>;
   static_assert(STAGES >= 4, "a round's tile is asked for two rounds before its map is formed, one round ahead");
-  static_assert(REC_THREADS == 4 * COLS && 32 * VEC == COLS, "one thread joins the states of a channel, another sends its map");
+  static_assert(COLS <= REC_THREADS / 4 && 32 * VEC % COLS == 0, "one thread joins the states of a channel, one of another warp sends its map");
+  constexpr int GROUPS = Shape::GROUPS;
   extern __shared__ __align__(128) char stages[];
-  __shared__ __align__(16) float2 warp_map[2][REC_WARPS][COLS];      // (A, H) of a warp's tokens, of this round and of the next
-  __shared__ __align__(16) float entering[2][REC_WARPS][COLS];       // the state that enters a warp's tokens
+  __shared__ __align__(16) float2 group_map[2][GROUPS][COLS];       // (A, H) of a group's tokens, of this round and of the next
+  __shared__ __align__(16) float entering[2][GROUPS][COLS];         // the state that enters a group's tokens
   __shared__ __align__(8) float2 tile_map[2][REC_MAX_CLUSTER][COLS];
   __shared__ uint64_t full[STAGES], maps_in[2];
   const cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int channel = tid % COLS;      // whose states (two warps) or maps (two others) this thread joins
-  const bool joins = tid < COLS, sends = tid / COLS == 2;
+  const int tid = threadIdx.x, lane = tid % (COLS / VEC), group = tid / (COLS / VEC);
+  const int channel = tid % COLS;      // whose states or maps this thread joins
+  const bool joins = tid < COLS, sends = tid >= REC_THREADS / 2 && tid < REC_THREADS / 2 + COLS;
   const int b = blockIdx.z, c0 = blockIdx.y * COLS;
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) tc::mbar_init(&full[i], 1);
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   float carry = joins && mine && begin ? begin[row + channel] : 0.f;
   bool lost = false;
   // this thread's first token (in the order of the recurrence) in a tile, and from one to the next
-  const int place = (BACK ? Shape::TOKENS - 1 - warp * STEPS : warp * STEPS) * COLS + lane * VEC;
+  const int place = (BACK ? Shape::TOKENS - 1 - group * STEPS : group * STEPS) * COLS + lane * VEC;
   constexpr int WAY = BACK ? -COLS : COLS;
 
   // A thread's tokens of a round: gates and rows from the time that their map is formed until they are gone over again.
@@ -239,17 +240,17 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) H = states(k, std::true_type(), make_float2(0.f, 0.f), nothing);
       if (lost) H = make_float2(NAN, NAN);
     }
-    *reinterpret_cast<float4*>(&warp_map[round & 1][warp][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
+    *reinterpret_cast<float4*>(&group_map[round & 1][group][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
   };
   // This CTA's map of a round to all ranks.  (It is what all threads issue together that counts: with the maps and states of a channel
   // joined by two threads each, or by four in all warps alike, 64 K tokens took 171 and 188 us.)
   const auto publish = [&](int round) {
     if (!sends || ranks == 1) return;
     const int turn = round & 1;
-    float2 m = warp_map[turn][0][channel];
+    float2 m = group_map[turn][0][channel];
 #pragma unroll
-    for (int w = 1; w < REC_WARPS; ++w) {
-      const float2 n = warp_map[turn][w][channel];
+    for (int w = 1; w < GROUPS; ++w) {
+      const float2 n = group_map[turn][w][channel];
       m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
     }
     if (channel == 0) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
@@ -274,9 +275,9 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       if (lost) state = carry = NAN;
     }
 #pragma unroll
-    for (int w = 0; w < REC_WARPS; ++w) {
+    for (int w = 0; w < GROUPS; ++w) {
       entering[turn][w][channel] = state;
-      const float2 m = warp_map[turn][w][channel];
+      const float2 m = group_map[turn][w][channel];
       state = rec_step(m.x, state, m.y);
     }
     if (ranks == 1) carry = state;
@@ -287,8 +288,8 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     char* xs = stage + place * sizeof(TX);
     char* as = stage + Shape::A_AT + place * sizeof(TA);
     const char* hs = stage + Shape::H_AT + place * sizeof(TX);
-    const float2 from = *reinterpret_cast<const float2*>(&entering[round & 1][warp][lane * VEC]);
-    const bool first = BACK && token_of(round) == 0 && warp == REC_WARPS - 1;      // token 0 is this thread's last
+    const float2 from = *reinterpret_cast<const float2*>(&entering[round & 1][group][lane * VEC]);
+    const bool first = BACK && token_of(round) == 0 && group == GROUPS - 1;      // token 0 is this thread's last
     const auto go = [&](auto closed) {
       [[maybe_unused]] constexpr bool CLOSED = decltype(closed)::value;
       const float2 none = make_float2(0.f, 0.f);
@@ -360,9 +361,9 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   if (end && rank == 0 && mine && tid < COLS) end[row + tid] = carry;
 }
 
-template <typename TX, typename TA, int STEPS, int STAGES, bool BACK>
+template <typename TX, typename TA, int COLS, int STEPS, int STAGES, bool BACK>
 cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
-  using Shape = Tile<TX, TA, STEPS, BACK>;
+  using Shape = Tile<TX, TA, COLS, STEPS, BACK>;
   Maps maps{};
   const auto make = [&](CUtensorMap* m, const void* data, const RowStride& s, int bytes) {
     return smat_make_map_rows(m, data, bytes, (uint64_t)a.channels, (uint64_t)a.T, (uint64_t)batch, (uint64_t)s.token * bytes,
@@ -371,7 +372,7 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   if (!make(&maps.x, a.x, a.xs, sizeof(TX)) || !make(&maps.log_a, a.log_a, a.as, sizeof(TA)) || !make(&maps.out, a.out, a.os, sizeof(TX)))
     return cudaErrorInvalidValue;
   if (BACK && (!make(&maps.h, a.h, a.hs, sizeof(TX)) || !make(&maps.dlog_a, a.dlog_a, a.das, sizeof(TA)))) return cudaErrorInvalidValue;
-  const auto kernel = recurrence_tma_kernel<TX, TA, STEPS, STAGES, BACK>;
+  const auto kernel = recurrence_tma_kernel<TX, TA, COLS, STEPS, STAGES, BACK>;
   constexpr size_t bytes = (size_t)STAGES * Shape::BYTES;
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (err != cudaSuccess) return err;
@@ -379,6 +380,23 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   const unsigned ranks = rec_ranks(columns, batch, tiles);
   return smat_launch_pdl_cluster(kernel, dim3(ranks, (unsigned)columns, (unsigned)batch), REC_THREADS, bytes, ranks, st, maps, a.begin, a.h0, a.end,
                                  (int)a.T, a.channels);
+}
+
+template <typename TX, typename TA, int STEPS, int STAGES, bool BACK>
+cudaError_t narrow(const RecArgs& a, int batch, int cols, cudaStream_t st) {
+  static_assert(STEPS % 2 == 1, "the groups of a warp read different banks");
+  return cols == 32 ? launch<TX, TA, 32, STEPS, STAGES, BACK>(a, batch, st) : launch<TX, TA, 16, STEPS, STAGES, BACK>(a, batch, st);
+}
+
+// Channels of a tile.  A long sequence of few channels leaves SMs idle with 64 (a line of bf16): with 32 or 16, whose rows are half and a
+// quarter of a line, a CTA has two and four times as many tokens a tile, and more CTAs run, as long as they all run at once (clusters
+// of eight: 32 of them; with 36 a second wave came, and 190 us where 64 channels take 157).  64 K tokens of bf16, forward and
+// backward, in us, with 64, 32, 16:       512 channels  120, 184   101, 141    82, 97
+//                                        1024 channels  143, 213   103, 143   128, 178
+// and 1024 tokens of 512 channels 3.9, 5.1   4.3, 4.8   5.2, 5.5.
+int rec_cols(const RecArgs& a, int batch) {
+  const int64_t columns = (a.channels + 63) / 64 * batch;
+  return a.T < 2048 || columns > 16 ? 64 : columns > 8 ? 32 : 16;
 }
 
 }  // namespace
@@ -395,11 +413,24 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
   return fits(a.x, a.xs, x) && fits(a.log_a, a.as, g) && fits(a.out, a.os, x) && (!back || (fits(a.h, a.hs, x) && fits(a.dlog_a, a.das, g)));
 }
 
-// Stages and tokens of a tile: two CTAs an SM, with two tiles or more on their way.  (One CTA of tiles three times as long issues half
-// the instructions a token, but eight warps an SM do not hide their latency: 64 K tokens 260 us.)
+// Tokens of a thread and stages: as many as two CTAs an SM have room for, and five stages or more (with four a tile comes late: gradients
+// of 64 K tokens with fp32 gates 341 us with <4, 5>, 461 with <5, 4>).  In between, more tokens a round pay where eight CTAs hand the
+// states on (32 K of fp32: <4, 5> 158 us, <3, 7> 168; gradients <2, 7> 264, <3, 5> 220), more stages where one or two do (4 x 8 K: 149 and
+// 138).  (One CTA an SM with tiles three times as long issues half the instructions a token, but eight warps do not hide their
+// latency: 64 K tokens 260 us.)
 cudaError_t smat_launch_recurrence_tma(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back, cudaStream_t st) {
   using bf16 = __nv_bfloat16;
-  if (!x_bf16) return back ? launch<float, float, 2, 7, true>(a, batch, st) : launch<float, float, 4, 5, false>(a, batch, st);
-  if (gate_bf16) return back ? launch<bf16, bf16, 6, 5, true>(a, batch, st) : launch<bf16, bf16, 8, 5, false>(a, batch, st);
-  return back ? launch<bf16, float, 4, 5, true>(a, batch, st) : launch<bf16, float, 4, 7, false>(a, batch, st);
+  const int cols = rec_cols(a, batch);
+  if (cols < 64) {
+    if (!x_bf16) return back ? narrow<float, float, 3, 5, true>(a, batch, cols, st) : narrow<float, float, 3, 7, false>(a, batch, cols, st);
+    if (gate_bf16) return back ? narrow<bf16, bf16, 5, 6, true>(a, batch, cols, st) : narrow<bf16, bf16, 7, 6, false>(a, batch, cols, st);
+    return back ? narrow<bf16, float, 3, 7, true>(a, batch, cols, st) : narrow<bf16, float, 5, 6, false>(a, batch, cols, st);
+  }
+  if (!x_bf16) {
+    if (back) return launch<float, float, 64, 3, 5, true>(a, batch, st);
+    const int64_t columns = (a.channels + 63) / 64;
+    return columns * batch * 4 > REC_CTAS ? launch<float, float, 64, 3, 7, false>(a, batch, st) : launch<float, float, 64, 4, 5, false>(a, batch, st);
+  }
+  if (gate_bf16) return back ? launch<bf16, bf16, 64, 6, 5, true>(a, batch, st) : launch<bf16, bf16, 64, 9, 5, false>(a, batch, st);
+  return back ? launch<bf16, float, 64, 4, 5, true>(a, batch, st) : launch<bf16, float, 64, 6, 5, false>(a, batch, st);
 }

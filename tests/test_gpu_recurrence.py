@@ -175,6 +175,44 @@ def test_strides_and_outputs_in_place():
 
 
 @pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("B,T,C", [(1, 2047, 512), (1, 2048, 512), (1, 2049, 520), (1, 4101, 1000), (1, 3000, 1032), (2, 3001, 264), (16, 2500, 24),
+                                   (1, 9000, 8), (8, 2300, 72), (130, 600, 64), (40, 2100, 72)])
+def test_few_channels(B, T, C, types):
+    """Tiles of 64, 32 and 16 channels, the last ones in part beyond the row."""
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, B + T + C, 100.0)
+    room = torch.full((B, T, C + 8), 5.0, dtype=types[0], device=DEV)
+    H, _ = check_forward(x, log_a, h0, H=room[..., :C])
+    assert bool((room[..., C:] == 5).all())
+    check_forward(x, log_a)
+    dH = torch.randn(B, T, C, generator=g, device=DEV).to(types[0])
+    check_backward(log_a, H, dH, h0, dhT)
+    check_backward(log_a, H, dH)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("C", [96, 520, 2048])
+def test_closed_gates_of_long_sequences(C, types):
+    B, T = 1, 2600
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, 13, 100.0)
+    log_a[:, [0, 1, 300, 301, 1500, 2599]] = -math.inf
+    H, hT = check_forward(x, log_a, h0)
+    dH = torch.randn(B, T, C, generator=g, device=DEV).to(types[0])
+    check_backward(log_a, H, dH, h0, dhT)
+    bad, hbad = x.clone(), H.clone()
+    bad[:, 310:1500:7] = math.nan
+    hbad[:, 301:1499] = math.inf
+    dbad = dH.clone()
+    dbad[:, 301:1400] = math.nan
+    other, last = b.recurrence_forward(bad, log_a, h0=h0)
+    assert torch.equal(other[:, :310], H[:, :310]) and torch.equal(other[:, 1500:], H[:, 1500:]) and torch.equal(last, hT)
+    want = b.recurrence_backward(log_a, H, dH, h0=h0, dhT=dhT)
+    got = b.recurrence_backward(log_a, hbad, dbad, h0=h0, dhT=dhT)
+    for p, q in zip(got[:2], want):
+        assert torch.equal(p[:, :301], q[:, :301]) and torch.equal(p[:, 1501:], q[:, 1501:])
+    assert torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("B,T,C", [(1, 15, 136), (1, 17, 2048), (300, 32, 132), (300, 33, 132), (300, 63, 131), (300, 65, 132), (2000, 20, 65),
                                    (1200, 104, 132), (1200, 105, 132), (1200, 207, 132), (1200, 209, 132)])
 def test_many_sequences(B, T, C, types):
