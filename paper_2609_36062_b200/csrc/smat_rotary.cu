@@ -13,7 +13,7 @@
 namespace {
 
 constexpr int ROT_THREADS = 256, ROT_UNROLL = 4;
-constexpr uint32_t ROT_CTAS = 148 * 4 * 6;   // six times as many as run at once
+constexpr uint32_t ROT_CTAS = 148 * 4 * 6;   // six times as many as run at once (fp32 gradients of 4 x 5056: 57 us, with one time 61)
 
 struct RotaryArgs {
   const void* x[2];
@@ -165,7 +165,7 @@ extern "C" smat_status smat_rotary(const smat_rotary_problem* p, const smat_rows
   a.positions_batch = p->positions_batch;
   a.first = p->first;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  // pieces of 16 bytes, pairs of elements, or one at a time
+  // pieces of 16 bytes, pairs of elements, or one at a time (90 of 128 columns turned: 120 us where 96 take 47)
   const auto moves = [&](int vec) {
     const unsigned bytes = (unsigned)(vec * dtype_bytes(p->dtype));
     return p->d % vec == 0 && p->rotated % (2 * vec) == 0 && rows_at_multiples(q, p->dtype, p->batch, p->q_heads, p->T, bytes) &&
