@@ -130,6 +130,8 @@ def stage_table(T, c, r, p, e, geo, u_bytes=4, f_bytes=4, alu_path=False) -> dic
         "tabulate_bf16": Work(0, geo.nnzC * rp, P * sf + B * su),
         "read_type":   Work(2 * m * rp, 0, m * r * e + B * st + m * p * 4),
         "read_type_tc": Work(2 * m * rp, 0, m * r * e + B * su + m * p * 2),
+        # the type table of a decode cache (d = 1: its one state) to codes of 8 bits and an fp32 unit a row
+        "pack":        Work(0, 0, max(B, 1) * (su + rp + 4 * r)),
         # ... and without tables
         "read_lines":  lines(r + p, (m * r + n * (r + p)) * e, m * p * row),
         "bwd_dq_lines": lines(r + p, (m * p + n * (r + p)) * e, m * r * 2),
