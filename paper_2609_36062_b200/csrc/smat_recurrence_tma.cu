@@ -274,11 +274,17 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       carry = behind;
       if (lost) state = carry = NAN;
     }
+    // (eight maps at a time ahead of the stores, which the compiler does not move them across)
 #pragma unroll
-    for (int w = 0; w < GROUPS; ++w) {
-      entering[turn][w][channel] = state;
-      const float2 m = group_map[turn][w][channel];
-      state = rec_step(m.x, state, m.y);
+    for (int w = 0; w < GROUPS; w += 8) {
+      float2 m[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = group_map[turn][w + i][channel];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        entering[turn][w + i][channel] = state;
+        state = rec_step(m[i].x, state, m[i].y);
+      }
     }
     if (ranks == 1) carry = state;
   };
