@@ -344,9 +344,10 @@ template <typename TX, typename TA, int VEC, int LANES, int STEPS, bool BACK, ty
 cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   constexpr int COLS = LANES * VEC, TILE = REC_THREADS / LANES * STEPS;
   const int64_t columns = (a.channels + COLS - 1) / COLS, tiles = (a.T + TILE - 1) / TILE;
-  const unsigned ranks = rec_ranks(columns, batch, tiles);
-  return smat_launch_pdl_cluster(recurrence_kernel<TX, TA, VEC, LANES, STEPS, BACK, OFF>, dim3(ranks, (unsigned)columns, (unsigned)batch),
-                                 REC_THREADS, 0, ranks, st, a);
+  const auto kernel = recurrence_kernel<TX, TA, VEC, LANES, STEPS, BACK, OFF>;
+  static RecRoom room;
+  const unsigned ranks = rec_ranks(room, kernel, 0, columns, batch, tiles);
+  return smat_launch_pdl_cluster(kernel, dim3(ranks, (unsigned)columns, (unsigned)batch), REC_THREADS, 0, ranks, st, a);
 }
 
 template <typename TX, typename TA, int VEC, bool BACK>

@@ -12,8 +12,8 @@
 // ahead, so that a round hides their way.  What sends the map of round n + 1 comes after a barrier behind all reads of those of
 // round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
 //
-// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 161 us where their
-// bytes take 122 (0.76 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
+// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 153 us where their
+// bytes take 122 (0.80 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
 // round ahead and pairs of channels the first took 233 us.
 #include <type_traits>
 
@@ -383,7 +383,8 @@ cudaError_t launch(const RecArgs& a, int batch, cudaStream_t st) {
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (err != cudaSuccess) return err;
   const int64_t columns = (a.channels + COLS - 1) / COLS, tiles = (a.T + Shape::TOKENS - 1) / Shape::TOKENS;
-  const unsigned ranks = rec_ranks(columns, batch, tiles);
+  static RecRoom room;
+  const unsigned ranks = rec_ranks(room, kernel, bytes, columns, batch, tiles);
   return smat_launch_pdl_cluster(kernel, dim3(ranks, (unsigned)columns, (unsigned)batch), REC_THREADS, bytes, ranks, st, maps, a.begin, a.h0, a.end,
                                  (int)a.T, a.channels);
 }
@@ -395,14 +396,15 @@ cudaError_t narrow(const RecArgs& a, int batch, int cols, cudaStream_t st) {
 }
 
 // Channels of a tile.  A long sequence of few channels leaves SMs idle with 64 (a line of bf16): with 32 or 16, whose rows are half and a
-// quarter of a line, a CTA has two and four times as many tokens a tile, and more CTAs run, as long as they all run at once (clusters
-// of eight: 32 of them; with 36 a second wave came, and 190 us where 64 channels take 157).  64 K tokens of bf16, forward and
-// backward, in us, with 64, 32, 16:       512 channels  120, 184   101, 141    82, 97
-//                                        1024 channels  143, 213   103, 143   128, 178
-// and 1024 tokens of 512 channels 3.9, 5.1   4.3, 4.8   5.2, 5.5.
+// quarter of a line, a CTA has two and four times as many tokens a tile, and more CTAs run.  16 K tokens of bf16, forward and backward,
+// in us, with 64, 32, 16:   512 channels  27, 40   22, 30   16, 23        704 channels  27, 41   22, 31   19, 25
+//                          1024 channels  36, 51   24, 34   25, 34       1728 channels  39, 55   34, 46   43, 62
+//                          2048 channels  42, 59   40, 57   43, 63,
+// and 512 tokens of 512 channels 2.8, 3.6   3.3, 3.5   3.8, 3.2.  (fp32: 704 channels 57, 75   40, 49   31, 40; 2048  77, 105   69, 107
+// 75, 107.)
 int rec_cols(const RecArgs& a, int batch) {
   const int64_t columns = (a.channels + 63) / 64 * batch;
-  return a.T < 2048 || columns > 16 ? 64 : columns > 8 ? 32 : 16;
+  return a.T < 2048 || columns > 28 ? 64 : columns > 11 ? 32 : 16;
 }
 
 }  // namespace

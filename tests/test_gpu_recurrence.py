@@ -176,9 +176,10 @@ def test_strides_and_outputs_in_place():
 
 @pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("B,T,C", [(1, 2047, 512), (1, 2048, 512), (1, 2049, 520), (1, 4101, 1000), (1, 3000, 1032), (2, 3001, 264), (16, 2500, 24),
-                                   (1, 9000, 8), (8, 2300, 72), (130, 600, 64), (40, 2100, 72)])
+                                   (1, 9000, 8), (8, 2300, 72), (130, 600, 64), (40, 2100, 72),
+                                   (1, 1500, 2304), (1, 1100, 2760), (1, 1300, 3201), (3, 700, 1608), (1, 2500, 1728)])
 def test_few_channels(B, T, C, types):
-    """Tiles of 64, 32 and 16 channels, the last ones in part beyond the row."""
+    """Tiles of 64, 32 and 16 channels, the last ones in part beyond the row; clusters of every size."""
     x, log_a, h0, dhT, g = inputs(B, T, C, types, B + T + C, 100.0)
     room = torch.full((B, T, C + 8), 5.0, dtype=types[0], device=DEV)
     H, _ = check_forward(x, log_a, h0, H=room[..., :C])
