@@ -13,7 +13,7 @@
 // round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
 //
 // Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 153 us where their
-// bytes take 122 (0.80 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 170 of 143 (0.84); without TMA, maps a
+// bytes take 122 (0.80 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 168 of 143 (0.85); without TMA, maps a
 // round ahead and pairs of channels the first took 233 us.
 #include <type_traits>
 
