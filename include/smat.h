@@ -374,9 +374,10 @@ smat_status smat_decode_step_gated(const smat_plan* plan, const void* q, const v
                                    int64_t t, void* o, void* cache, size_t cache_bytes, void* cuda_stream);
 
 /* ---- Decode cache with its type table in 8 bits (Sec. "Memory-efficient decoding": the B type states are nearly all of it) ----
- * A row U_h[i, :] of d_v entries is kept as int8 codes and one fp32 unit: with m = 127 / max_j |U_h[i, j]| in fp32, cut to eight
- * significant bits (at most 2^126), code = U m rounded to the nearest whole number (even between two), value = code * unit,
- * unit = 1 / m (no larger than the element type's largest number).  A row of zeros has unit 0; a row with an entry that is not finite has unit NaN (all of its values are NaN).
+ * A row U_h[i, :] of d_v entries is kept as int8 codes and one fp32 unit: with m the largest number of eight significant bits, at most
+ * 2^126, for which m max_j |U_h[i, j]| <= 127 (exactly, not as a rounded quotient), code = U m rounded to the nearest whole number (even
+ * between two), unit = 1 / m in fp32, value = code * unit, at most the element type's largest number.  A row of zeros has unit 0; a row
+ * with an entry that is not finite has unit NaN (all of its values are NaN).
  *
  * packed: device memory owned by the caller, 256-byte aligned, smat_decode_packed_bytes(plan) bytes: the codes
  *        [B*H][B][d_k][d_v] int8, the units [B*H][B][d_k] fp32, then S and (gated plans) log g as in the decode cache; each

@@ -1,7 +1,9 @@
-// Type table of the decode cache in 8 bits, and back.  A row of p entries gets m = 127 / max|row|, cut to the eight significant bits of
-// a bf16 number: code = entry * m rounded to the nearest whole number (even between two), value = code * (1 / m).  With eight bits in m the
-// product is exact in twice the entry's bits, so a code is the nearest one in any arithmetic; the cut costs less than 2^-7 of the
-// range.  A code's value is off by at most half a unit, max|row| / 254 (1 + 2^-7).
+// Type table of the decode cache in 8 bits, and back.  A row of p entries gets the largest m of eight significant bits (a bf16 number)
+// with m max|row| <= 127: code = entry * m rounded to the nearest whole number (even between two), value = code * (1 / m).  With eight
+// bits in m both products are exact in twice the entry's bits, so that m and the codes are the same in any arithmetic; a quotient 127 / max
+// that is rounded before it is cut to eight bits is not (next to such a number it takes the step of 2^-7 to the other side: 8 rows in a
+// million of fp32, every code of the row another).  The cut costs less than 2^-7 of the range.  A code's value is off by at most half
+// a unit, max|row| / 254 (1 + 2^-7).
 //
 // Streams: a row is held by the lanes that read it in 16-byte pieces (p = 128 of bf16: 16 lanes, 8 codes each), its largest entry
 // found by shuffles.  PACK_ROWS rows are in flight a thread.  Packing is bound by HBM only with few instructions an entry: with a
@@ -59,7 +61,12 @@ __global__ void __launch_bounds__(PACK_THREADS) pack_kernel(const TU* table, int
     for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool finite = top < 0x7f800000u;
     float m = 0.f;
-    if (top != 0u && finite) m = __uint_as_float(__float_as_uint(fminf(__fdiv_rn(127.f, __uint_as_float(top)), 0x1p126f)) & 0xffff0000u);
+    if (top != 0u && finite) {
+      const float most = __uint_as_float(top);
+      uint32_t bits = __float_as_uint(fminf(__fdiv_rn(127.f, most), 0x1p126f)) & 0xffff0000u;
+      if (fmaf(__uint_as_float(bits), most, -127.f) > 0.f) bits -= 0x10000u;      // rounded up to it: one step of the eighth bit less
+      m = __uint_as_float(bits);
+    }
     // entry * m + 1.5 * 2^23: the product is exact inside the fused operation, and the sum's one rounding is that to a whole number
     uint32_t word[VEC / 4];
     const float2 mm = make_float2(m, m), whole = make_float2(12582912.f, 12582912.f);

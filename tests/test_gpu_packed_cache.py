@@ -1,6 +1,7 @@
 """Decode cache with its type table in 8 bits on the GPU: the codes bit for bit, the steps against 64 bits, against the steps on the
 cache that it was packed from, and against the dense mask."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -277,3 +278,42 @@ def test_captured_steps_and_refusals():
         plan.decode_step_packed(*row, n, one, log_a_t=torch.zeros(2, device="cuda"))
     with pytest.raises(b.SmatError):
         plan.decode_pack(one)                              # a packed cache is shorter than a cache
+
+
+def largest_multiplier(top):
+    """The largest number of eight significant bits, at most 2^126, whose product with `top` is at most 127: in whole numbers."""
+    t, most = Fraction(top), Fraction(2) ** 126
+    if t * most <= 127:
+        return float(most) if t else 0.0
+    q = Fraction(127) / t
+    e = -200
+    while Fraction(2) ** (e + 8) <= q:
+        e += 1
+    return float((q / Fraction(2) ** e).__floor__() * Fraction(2) ** e)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_whose_multiplier_is_next_to_a_border(dtype):
+    """127 / max within a rounding of fp32 of a number of eight bits: whichever way a quotient in fp32 falls there, the multiplier is the
+    largest one that keeps the codes within 127."""
+    plan = b.SmatPlan(1, 1, 1024, 128, 128, 2, 128, dtype)
+    cache = torch.zeros_like(plan.decode_cache())
+    t = Cache(plan, cache, False).table
+    rows = t.view(-1, 128)
+    tops = []
+    for eighth in range(128, 256):
+        near = np.float32(127.0 / eighth)
+        for top in (np.nextafter(near, np.float32(0)), near, np.nextafter(near, np.float32(9))):
+            tops += [float(top), float(top) * 2.0 ** -31, float(top) * 2.0 ** 90]
+    tops += [127.0 * 2.0 ** k for k in (-133, -40, 0, 100)] + [2.0 ** k for k in (-149, -130, -126, -3, 127)]
+    assert len(tops) <= rows.shape[0]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    top = torch.tensor(tops, dtype=torch.float64, device="cuda")
+    entries = (top[:, None] * (2 * torch.rand(len(tops), 128, generator=g, device="cuda", dtype=torch.float64) - 1)).to(t.dtype)
+    entries[:, 5] = top.to(t.dtype)
+    rows[:len(tops)] = entries
+    m = torch.tensor([largest_multiplier(x) for x in entries.double().abs().amax(-1).tolist()], dtype=torch.float64, device="cuda")
+    v = Cache(plan, plan.decode_pack(cache), True)
+    codes, unit = v.codes.view(-1, 128)[:len(tops)], v.unit.view(-1)[:len(tops)]
+    assert torch.equal(codes.double(), torch.round(entries.double() * m[:, None]))
+    assert torch.equal(unit, torch.where(m > 0, 1 / m, torch.zeros_like(m)).float())
