@@ -317,3 +317,30 @@ def test_rows_whose_multiplier_is_next_to_a_border(dtype):
     codes, unit = v.codes.view(-1, 128)[:len(tops)], v.unit.view(-1)[:len(tops)]
     assert torch.equal(codes.double(), torch.round(entries.double() * m[:, None]))
     assert torch.equal(unit, torch.where(m > 0, 1 / m, torch.zeros_like(m)).float())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("case", CASES)
+def test_steps_on_the_unpacked_cache(case, gated):
+    """A step on a packed cache and on the cache that it unpacks to: the same running state bit for bit, and outputs that differ by the
+    values' rounding to the table's type (a packed one is code * unit, not rounded), and by that of the sums."""
+    w, _, dev, plan, la = make(case, gated)
+    packed = plan.decode_pack(begin(plan, dev, la))
+    cache = plan.decode_unpack(packed)
+    v, u = Cache(plan, packed, True), Cache(plan, cache, False)
+    geo, bh = plan.geometry(), w.bh
+    value = 2.0 ** -8 if u.table.dtype == torch.bfloat16 else 2.0 ** -24
+    half = 2.0 ** -8 if case[5] == "bf16" else 2.0 ** -24
+    for i in range(min(geo.m, 16)):
+        t = geo.n + i
+        row = [dev[n][:, :, t].contiguous() for n in "qkv"]
+        lt = la[:, t].contiguous() if gated else None
+        one = plan.decode_step_packed(*row, t, packed, log_a_t=lt)
+        two = plan.decode_step_gated(*row, lt, t, cache) if gated else plan.decode_step(*row, t, cache)
+        assert torch.equal(v.S, u.S) and (not gated or torch.equal(v.log_g, u.log_g))
+        q = row[0].double().abs().view(bh, -1)
+        U = u.table[:, (i + 1) % geo.B].double().abs()
+        # of the packed side: the unit's product with the gate's factor; of both: a fused sum an entry, and d_k products in turn
+        bound = torch.einsum("hi,hij->hj", q, U * (value + 2.0 ** -23) + (U + v.S.double().abs()) * 2 * (w.d_k + 2) * 2.0 ** -24)
+        off = (one.double() - two.double()).abs().view(bh, -1) - (half * (one.double().abs() + two.double().abs()).view(bh, -1) + bound)
+        assert float(off.max()) <= 0.0, (t, float(off.max()))
