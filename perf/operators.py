@@ -145,11 +145,13 @@ def _doubled(a, x):
 
 
 def _codes(U):
-    """Rows in 8 bits: codes x m rounded to even with m = 127 / max|x| cut to eight significant bits, so that a product with a
-    bf16 entry is exact and a value between two codes is the same in any arithmetic; and what a code counts, 1 / m in fp32."""
-    top = U.abs().amax(-1, keepdim=True).float()
-    m = torch.where(top > 0, (127.0 / top).clamp(max=2.0 ** 126), torch.zeros_like(top))
-    m = (m.contiguous().view(torch.int32) & -65536).view(torch.float32)
+    """Rows in 8 bits: codes x m rounded to even with m the largest number of eight significant bits for which m max|x| <= 127, so
+    that a product with an entry is exact and m and the codes are the same in any arithmetic; and what a code counts, 1 / m in fp32.
+    The quotient is taken in 64 bits, where a largest entry of 24 bits leaves it on its side of every number of eight bits;
+    an fp32 quotient, or the reciprocal times 127, is rounded onto some of them."""
+    top = U.abs().amax(-1, keepdim=True).double()
+    m = torch.where(top > 0, torch.div(torch.full_like(top, 127.0), top).clamp(max=2.0 ** 126), torch.zeros_like(top))
+    m = (m.contiguous().view(torch.int64) & -(1 << 45)).view(torch.float64).float()
     wide = U.float() if U.dtype == torch.bfloat16 else U.double()
     return torch.round(wide * m).to(torch.int8), torch.where(m > 0, 1.0 / m, torch.zeros_like(m)).float()
 
