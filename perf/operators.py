@@ -236,7 +236,7 @@ def _prepare_packed(case, st, normal, uniform, dtype):
     if not own:
         st.update(U=U, S=S, log_g=log_g)
         if case["mode"] == "step":
-            st["codes"], st["unit"] = _codes(st.pop("U"))
+            st["codes"], st["unit"] = _codes(U)
         return
     cache = plan.decode_cache()
     pad = lambda n: (n + 255) // 256 * 256
@@ -534,19 +534,24 @@ def _exact_recurrence(case, st):
     return {"dx": g, "dlog_a": g * a * before, "dh0": g[:, 0] * a[:, 0]}
 
 
+def _exact_codes(U):
+    """Codes and multipliers of the rows of U: floor to eight significant bits of the quotient, rounding to even, in 64 bits."""
+    quotient = 127 / U.abs().amax(-1, keepdim=True).double()
+    bits = 2.0 ** (7 - torch.floor(torch.log2(quotient)))
+    m = torch.floor(quotient * bits) / bits
+    return torch.round(U.double() * m), m
+
+
 def _exact_packed(case, st):
     if case["mode"] == "write":
-        # whole multiples of the unit of a row, the nearest one (the even one between two)
-        U = st["U"]
-        if U.numel() > 1 << 29:
+        if st["U"].numel() > 1 << 29:
             return None
-        top = U.abs().amax(-1, keepdim=True).double()
-        m = torch.floor(127 / top * 2.0 ** (7 - torch.floor(torch.log2(127 / top)))) / 2.0 ** (7 - torch.floor(torch.log2(127 / top)))
-        return {"U": (torch.round(U.double() * m) / m), "S": st["S"].double()}
+        codes, m = _exact_codes(st["U"])
+        return {"U": codes / m, "S": st["S"].double()}
     j = 0
     q, k, v = (st[x][j].double() for x in "qkv")
-    t = 1 % st["types"]
-    U = (st["codes"][:, t].double() * st["unit"][:, t].double()).view(st["S"].shape)
+    codes, m = _exact_codes(st["U"][:, 1 % st["types"]])
+    U = (codes / m).view(st["S"].shape)
     S, log_g = st["S"].double(), None
     if case["gated"]:
         log_g = st["log_g"].double() + st["a"][j].double()
