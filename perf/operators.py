@@ -370,12 +370,12 @@ def _run_plain(st):
             st["state"].mul_(a[:, 0]).add_(st["x"][:, 0].float())
             return {"h": st["state"][:, None].to(dtype), "state": st["state"]}
         if case["mode"] == "forward":
-            x = st["x"].float().clone()      # (a tensor of fp32 is its own .float())
+            x = st["x"].to(torch.float32, copy=True)      # (a tensor of fp32 is its own .float())
             x[:, 0] += a[:, 0] * st["h0"]
             h = _doubled(a, x)
             return {"h": h.to(dtype), "last": h[:, -1].clone()}
         # c_t = a_t (dh_t + c_{t+1}), c_T = dhT; dx_t = dh_t + c_{t+1}, dlog_a_t = c_t h_{t-1}, dh0 = c_0
-        dh = st["dh"].float().clone()
+        dh = st["dh"].to(torch.float32, copy=True)
         dh[:, -1] += st["dhT"]
         c = _doubled(a.flip(1), (a * dh).flip(1)).flip(1)
         before = torch.cat((st["h0"][:, None], st["h"][:, :-1].float()), 1)
