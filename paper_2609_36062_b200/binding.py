@@ -280,6 +280,8 @@ def measure_fadd_rate(packed: bool = False, stream=None) -> float:
 
 
 # -- operators around the pass ---------------------------------------------------------------------
+# A call on a stream that is given (stream=), and not the current one, takes the memory of its new outputs and of its workspace from that
+# stream.  The caller makes either stream wait for the other as for any kernel; outputs may be given back while either uses them.
 def rotary_frequencies(rotated: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0, trained_length: int = 4096,
                        fast_turns: float = 32.0, slow_turns: float = 1.0, device="cuda"):
     """(frequencies, scale) for rotary(): radians a token of every pair, base ** (-2 i / rotated), as an fp64 tensor, and the
@@ -512,15 +514,26 @@ class SmatPlan:
     def decode_cache_packed(self, device="cuda") -> torch.Tensor:
         return torch.empty(int(self.lib.smat_decode_packed_bytes(self.handle)), dtype=torch.uint8, device=device)
 
+    @staticmethod
+    def _taken_on(stream, make, device) -> torch.Tensor:
+        """make(device) for a call on `stream`: memory of that stream, which the caller's may use too."""
+        caller = torch.cuda.current_stream(device) if stream is not None else None
+        if caller is None or stream.cuda_stream == caller.cuda_stream:
+            return make(device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream.cuda_stream, device) if stream.cuda_stream else torch.cuda.default_stream(device)):
+            taken = make(device)
+        taken.record_stream(caller)
+        return taken
+
     def decode_pack(self, cache, packed=None, stream=None) -> torch.Tensor:
         """smat_decode_pack: the packed form of a decode cache."""
-        packed = self.decode_cache_packed(cache.device) if packed is None else packed
+        packed = self._taken_on(stream, self.decode_cache_packed, cache.device) if packed is None else packed
         self._native.repack(cache, packed, stream, True)
         return packed
 
     def decode_unpack(self, packed, cache=None, stream=None) -> torch.Tensor:
         """smat_decode_unpack: the decode cache that a packed one stands for."""
-        cache = self.decode_cache(packed.device) if cache is None else cache
+        cache = self._taken_on(stream, self.decode_cache, packed.device) if cache is None else cache
         self._native.repack(cache, packed, stream, False)
         return cache
 

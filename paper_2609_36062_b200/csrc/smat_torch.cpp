@@ -14,6 +14,7 @@
 
 #include <exception>
 #include <initializer_list>
+#include <optional>
 #include <string>
 #include <vector>
 
@@ -349,25 +350,51 @@ bool float_type(PyObject* o, const char* name, at::ScalarType* dtype) {
 }
 smat_dtype smat_type(at::ScalarType t) { return t == at::kBFloat16 ? SMAT_BF16 : SMAT_F32; }
 
-// A new contiguous tensor on the device of `like`, which is the current one.  (Straight from the allocator's front end: two outputs through
-// the dispatcher cost a single-token call 1 us of 5.)
-at::Tensor fresh(at::IntArrayRef shape, at::ScalarType dtype, const at::Tensor& like) {
-  return at::Tensor(at::detail::empty_cuda(shape, dtype, like.device(), c10::nullopt));
-}
+// Where a call runs: on the tensors' device, and on its current stream or on the one that is given.  A given stream is the
+// current one while the call takes memory: what it takes belongs to that stream, so that a workspace is free again behind the kernels
+// that use it, and no block is written while the caller's stream still uses it for what it held before.
+struct Running {
+  c10::cuda::CUDAGuard device;
+  c10::cuda::OptionalCUDAStreamGuard given;
+  std::optional<c10::cuda::CUDAStream> caller;      // the caller's stream, where it is another
+  void* st = nullptr;
+
+  explicit Running(const at::Tensor& t) : device(t.device()) {}
+  bool on(PyObject* o) {
+    if (!stream(o, &st)) return false;
+    if (o == Py_None) return true;
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream();
+    if (st == current.stream()) return true;
+    caller = current;
+    given.reset_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), current.device_index()));
+    return true;
+  }
+  // A new contiguous tensor.  (Straight from the allocator's front end: two outputs through the dispatcher cost a single-token call
+  // 1 us of 5.)
+  at::Tensor fresh(at::IntArrayRef shape, at::ScalarType dtype) const {
+    return at::Tensor(at::detail::empty_cuda(shape, dtype, device.current_device(), c10::nullopt));
+  }
+  // ... that the caller gets, and may give back while its own stream reads it
+  at::Tensor output(at::IntArrayRef shape, at::ScalarType dtype) const {
+    at::Tensor t = fresh(shape, dtype);
+    if (caller) t.record_stream(caller->unwrap());
+    return t;
+  }
+};
 
 // An output: the caller's tensor (this shape, any strides), or a new contiguous one.
-bool rows_output(PyObject* o, const char* name, const at::Tensor& like, at::Tensor* out) {
+bool rows_output(PyObject* o, const char* name, const at::Tensor& like, const Running& run, at::Tensor* out) {
   if (o == Py_None) {
-    *out = fresh(like.sizes(), like.scalar_type(), like);
+    *out = run.output(like.sizes(), like.scalar_type());
     return true;
   }
   const at::Tensor* t = rows_tensor(o, name, like.scalar_type(), like.sizes(), &like);
   if (t) *out = *t;
   return t != nullptr;
 }
-bool array_output(PyObject* o, const char* name, at::IntArrayRef shape, const at::Tensor& like, at::Tensor* out) {
+bool array_output(PyObject* o, const char* name, at::IntArrayRef shape, const at::Tensor& like, const Running& run, at::Tensor* out) {
   if (o == Py_None) {
-    *out = fresh(shape, at::kFloat, like);
+    *out = run.output(shape, at::kFloat);
     return true;
   }
   const at::Tensor* t = array_tensor(o, name, at::kFloat, shape, like);
@@ -445,10 +472,9 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!fits_int(batch, "Q") || !fits_int(Q->size(1), "Q") || (K && !fits_int(K->size(1), "K")) || !fits_int(Q->size(-1), "Q") ||
         !fits_int(F->size(0) * 2, "frequencies"))
       return nullptr;
-    const c10::cuda::CUDAGuard guard(Q->device());
+    Running run(*Q);
     at::Tensor Qo, Ko;
-    void* st;
-    if (!rows_output(a[8], "Q_out", *Q, &Qo) || (K && !rows_output(a[9], "K_out", *K, &Ko)) || !stream(a[10], &st)) return nullptr;
+    if (!run.on(a[10]) || !rows_output(a[8], "Q_out", *Q, run, &Qo) || (K && !rows_output(a[9], "K_out", *K, run, &Ko))) return nullptr;
     p.batch = (int)batch;
     p.q_heads = (int)Q->size(1);
     p.k_heads = K ? (int)K->size(1) : 0;
@@ -464,7 +490,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const smat_rows q = rows_of(*Q, axes), qo = rows_of(Qo, axes);
     smat_rows k{}, ko{};
     if (K) { k = rows_of(*K, axes); ko = rows_of(Ko, axes); }
-    const int rc = unlocked([&] { return smat_rotary(&p, &q, K ? &k : nullptr, &qo, K ? &ko : nullptr, st); });
+    const int rc = unlocked([&] { return smat_rotary(&p, &q, K ? &k : nullptr, &qo, K ? &ko : nullptr, run.st); });
     if (!fail_status(rc, "smat_rotary")) return nullptr;
     return K ? wrap_all({Qo, Ko}) : wrap(Qo);
   } catch (...) {
@@ -519,16 +545,15 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[3] != Py_None && !(R = rows_tensor(a[3], "residual", dtype, X->sizes(), X))) return nullptr;
     if (a[5] != Py_None && !(G = rows_tensor(a[5], "gate", dtype, X->sizes(), X))) return nullptr;
     const bool keeps = R || S || a[8] != Py_None;
-    const c10::cuda::CUDAGuard guard(X->device());
+    Running run(*X);
     at::Tensor Y, H;
-    void* st;
-    if (!rows_output(a[7], "Y", *X, &Y) || (keeps && !rows_output(a[8], "H", *X, &H)) || !stream(a[9], &st)) return nullptr;
+    if (!run.on(a[9]) || !rows_output(a[7], "Y", *X, run, &Y) || (keeps && !rows_output(a[8], "H", *X, run, &H))) return nullptr;
     const smat_rows x = rows_of(*X, axes), y = rows_of(Y, axes);
     smat_rows r{}, g{}, h{};
     if (R) r = rows_of(*R, axes);
     if (G) g = rows_of(*G, axes);
     if (keeps) h = rows_of(H, axes);
-    const int rc = unlocked([&] { return smat_norm_forward(&p, &x, R ? &r : nullptr, G ? &g : nullptr, &y, keeps ? &h : nullptr, st); });
+    const int rc = unlocked([&] { return smat_norm_forward(&p, &x, R ? &r : nullptr, G ? &g : nullptr, &y, keeps ? &h : nullptr, run.st); });
     if (!fail_status(rc, "smat_norm_forward")) return nullptr;
     return keeps ? wrap_all({Y, H}) : wrap(Y);
   } catch (...) {
@@ -558,17 +583,17 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
         (a[6] != Py_None && !(dI = rows_tensor(a[6], "dH", dtype, H->sizes(), H))) ||
         (S && !(X = rows_tensor(a[7], "X", dtype, H->sizes(), H))))
       return nullptr;
-    const c10::cuda::CUDAGuard guard(H->device());
+    Running run(*H);
     at::Tensor dH, dX, dG, dW, dS, own;
-    void *st, *ws = nullptr;
+    void* ws = nullptr;
     size_t bytes = smat_norm_workspace_bytes(&p);
-    if (!rows_output(a[9], "dH_out", *H, &dH) || (S && !rows_output(a[10], "dX", *H, &dX)) ||
-        (G && !rows_output(a[11], "dgate", *H, &dG)) || !stream(a[13], &st))
+    if (!run.on(a[13]) || !rows_output(a[9], "dH_out", *H, run, &dH) || (S && !rows_output(a[10], "dX", *H, run, &dX)) ||
+        (G && !rows_output(a[11], "dgate", *H, run, &dG)))
       return nullptr;
-    dW = fresh(W->sizes(), at::kFloat, *H);
-    if (S) dS = fresh(S->sizes(), at::kFloat, *H);
+    dW = run.output(W->sizes(), at::kFloat);
+    if (S) dS = run.output(S->sizes(), at::kFloat);
     if (a[12] == Py_None) {
-      own = fresh({(int64_t)bytes}, at::kByte, *H);
+      own = run.fresh({(int64_t)bytes}, at::kByte);
       ws = own.data_ptr();
     } else if (!workspace(a[12], "workspace", &ws, &bytes)) {
       return nullptr;
@@ -584,7 +609,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float *dw = dW.data_ptr<float>(), *ds = S ? dS.data_ptr<float>() : nullptr;
     const int rc = unlocked([&] {
       return smat_norm_backward(&p, &dy, &h, G ? &g : nullptr, S ? &x : nullptr, dI ? &di : nullptr, &dh, S ? &dx : nullptr,
-                                G ? &dg : nullptr, dw, ds, ws, bytes, st);
+                                G ? &dg : nullptr, dw, ds, ws, bytes, run.st);
     });
     if (!fail_status(rc, "smat_norm_backward")) return nullptr;
     PyObject* tuple = PyTuple_New(5);
@@ -629,14 +654,13 @@ PyObject* recurrence_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t state[2] = {p.batch, p.channels};
     const at::Tensor* h0 = nullptr;
     if (a[2] != Py_None && !(h0 = array_tensor(a[2], "h0", at::kFloat, state, *X))) return nullptr;
-    const c10::cuda::CUDAGuard guard(X->device());
+    Running run(*X);
     at::Tensor H, hT;
-    void* st;
-    if (!rows_output(a[3], "H", *X, &H) || !array_output(a[4], "hT", state, *X, &hT) || !stream(a[5], &st)) return nullptr;
+    if (!run.on(a[5]) || !rows_output(a[3], "H", *X, run, &H) || !array_output(a[4], "hT", state, *X, run, &hT)) return nullptr;
     const smat_rows x = rows_of(*X, axes), la = rows_of(*A, axes), h = rows_of(H, axes);
     const float* from = h0 ? h0->data_ptr<float>() : nullptr;
     float* to = hT.data_ptr<float>();
-    const int rc = unlocked([&] { return smat_recurrence_forward(&p, &x, &la, from, &h, to, st); });
+    const int rc = unlocked([&] { return smat_recurrence_forward(&p, &x, &la, from, &h, to, run.st); });
     return fail_status(rc, "smat_recurrence_forward") ? wrap_all({H, hT}) : nullptr;
   } catch (...) {
     return raise();
@@ -660,16 +684,15 @@ PyObject* recurrence_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if ((a[3] != Py_None && !(h0 = array_tensor(a[3], "h0", at::kFloat, state, *H))) ||
         (a[4] != Py_None && !(dhT = array_tensor(a[4], "dhT", at::kFloat, state, *H))))
       return nullptr;
-    const c10::cuda::CUDAGuard guard(H->device());
+    Running run(*H);
     at::Tensor dX, dA, dh0;
-    void* st;
-    if (!rows_output(a[5], "dX", *H, &dX) || !rows_output(a[6], "dlog_a", *A, &dA) || !array_output(a[7], "dh0", state, *H, &dh0) ||
-        !stream(a[8], &st))
+    if (!run.on(a[8]) || !rows_output(a[5], "dX", *H, run, &dX) || !rows_output(a[6], "dlog_a", *A, run, &dA) ||
+        !array_output(a[7], "dh0", state, *H, run, &dh0))
       return nullptr;
     const smat_rows la = rows_of(*A, axes), h = rows_of(*H, axes), dh = rows_of(*dH, axes), dx = rows_of(dX, axes), da = rows_of(dA, axes);
     const float *start = h0 ? h0->data_ptr<float>() : nullptr, *from = dhT ? dhT->data_ptr<float>() : nullptr;
     float* to = dh0.data_ptr<float>();
-    const int rc = unlocked([&] { return smat_recurrence_backward(&p, &la, &h, &dh, start, from, &dx, &da, to, st); });
+    const int rc = unlocked([&] { return smat_recurrence_backward(&p, &la, &h, &dh, start, from, &dx, &da, to, run.st); });
     return fail_status(rc, "smat_recurrence_backward") ? wrap_all({dX, dA, dh0}) : nullptr;
   } catch (...) {
     return raise();
