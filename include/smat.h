@@ -474,7 +474,8 @@ smat_status smat_norm_backward(const smat_norm_problem* problem, const smat_rows
  * x, log_a, h [batch, T, channels] (the head strides are not used); h0, hT [batch, channels] DEVICE fp32, contiguous: hT
  * (NULL: not wanted) receives h_{T-1}, unrounded, and may be h0, so that T = 1 is a decoding step.  log-gates <= 0 as in
  * smat_forward_gated, in gate_dtype (that of x, or fp32).  A closed gate (log_a = -inf) forgets all of what came before, values
- * that are not finite among it: with one at the first token of every sequence, packed sequences do not see one another.
+ * that are not finite among it: with one at the first token of every sequence, packed sequences do not see one another.  Open
+ * gates forget nothing that is not finite, however small their product.  (A gate that is zero in fp32, log_a below -104, is a closed one.)
  * The state is fp32.  h may be x.  (Kernels of long sequences wait for copies and for one another within a cluster; a wait that ran
  * out, after two seconds, leaves NaN in what follows.)
  * Backward: from dh (and dhT, the gradient at hT, NULL: none) and the h that was kept,

@@ -3,7 +3,7 @@
 // the same kind of recurrence from the last token to the first.  Below, s counts tokens in the order of the recurrence.
 //
 // Tokens s in a row map the state that enters them to the one that leaves them, state -> A state + H, and two such maps in a row
-// are one again: (A, H) then (A', H') is (A' A, A' H + H').  So a long sequence is cut into pieces whose maps are formed side by
+// are one again: (A, H) then (A', H') is (A' A, A' H + H') (A' A as rec_joined has it).  So a long sequence is cut into pieces whose maps are formed side by
 // side, joined in order, and applied: a CTA takes 64 channels (a line of 128 bytes of bf16) and walks over the tokens a tile at a time; in the
 // tile a thread has VEC channels of STEPS tokens in registers, forms their map, the maps meet by shuffles (a warp) and shared
 // memory (the CTA), and the thread goes over its tokens again from the state that enters them.  Every input is read once,
@@ -95,6 +95,14 @@ __device__ __forceinline__ void map_of(const Share<TX, TA, VEC, STEPS, BACK>& in
       A[i] *= gate[l][i];
       advance<CLOSED, BACK>(gate, l, i, in.x[l].get(i), v[i], H[i]);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    if (A[i] > 0.f) continue;
+    float least = gate[0][i];
+#pragma unroll
+    for (int l = 1; l < STEPS; ++l) least = fminf(least, gate[l][i]);
+    A[i] = rec_factor(A[i], least);
   }
 }
 
@@ -278,7 +286,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
           before_A[i] = a;
           before_H[i] = h;
           H[i] = rec_step(A[i], h, H[i]);
-          A[i] *= a;
+          A[i] = rec_joined(A[i], a);
         }
       }
     }
@@ -292,7 +300,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_kernel(const RecArg
 #pragma unroll
         for (int w = 1; w < REC_WARPS; ++w) {
           const float2 n = warp_map[w][tid];
-          m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
+          m = make_float2(rec_joined(n.x, m.x), rec_step(n.x, m.y, n.y));
         }
         for (int r = 0; r < ranks; ++r) *cluster.map_shared_rank(&tile_map[turn][rank][tid], r) = m;
       }

@@ -25,6 +25,15 @@ struct RecArgs {
 // a * state + x, a closed gate forgetting the state whatever it is.
 __device__ __forceinline__ float rec_step(float a, float state, float x) { return a == 0.f ? x : fmaf(a, state, x); }
 
+// The factor of a piece of tokens is the product of its gates, and zero only where one of them is closed: a product of open gates that
+// fp32 has no number for (nine of exp(-12)) is held at the smallest one, so that a state that is not finite stays so.  For a finite
+// state this is the error that products below 2^-126 have anyway, 2^-149 of it.  (A product with a gate that is NaN needs no care: what
+// that gate leaves is NaN by itself, until a closed one.)
+constexpr float REC_LEAST = 0x1p-149f;
+__device__ __forceinline__ float rec_factor(float product, float least_gate) { return fmaxf(product, fminf(least_gate, REC_LEAST)); }
+// ... of two pieces in a row.
+__device__ __forceinline__ float rec_joined(float later, float earlier) { return rec_factor(later * earlier, fminf(later, earlier)); }
+
 // Whether a sum of numbers times zero has met one that is not finite.  Only then does a closed gate need looking at (0 * state is
 // no zero): the loops over tokens run without it, and once more with it where what they come to is not finite.
 __device__ __forceinline__ bool rec_not_finite(float zeros) { return zeros != 0.f; }

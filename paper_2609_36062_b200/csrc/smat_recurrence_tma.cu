@@ -235,6 +235,12 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       open_gates(a, k.gate);
 #pragma unroll
       for (int l = 0; l < STEPS; ++l) A = __fmul2_rn(A, k.gate[l]);
+      if (!(A.x > 0.f && A.y > 0.f)) {
+        float2 least = k.gate[0];
+#pragma unroll
+        for (int l = 1; l < STEPS; ++l) least = make_float2(fminf(least.x, k.gate[l].x), fminf(least.y, k.gate[l].y));
+        A = make_float2(rec_factor(A.x, least.x), rec_factor(A.y, least.y));
+      }
       const auto nothing = [](int, float2, float2) {};
       H = states(k, std::false_type(), make_float2(0.f, 0.f), nothing);
       if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) H = states(k, std::true_type(), make_float2(0.f, 0.f), nothing);
@@ -251,7 +257,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
 #pragma unroll
     for (int w = 1; w < GROUPS; ++w) {
       const float2 n = group_map[turn][w][channel];
-      m = make_float2(n.x * m.x, rec_step(n.x, m.y, n.y));
+      m = make_float2(rec_joined(n.x, m.x), rec_step(n.x, m.y, n.y));
     }
     if (channel == 0) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
     for (int r = 0; r < ranks; ++r) send(in_rank(&tile_map[turn][rank][channel], r), in_rank(&maps_in[turn], r), m);

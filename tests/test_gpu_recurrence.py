@@ -335,3 +335,47 @@ def test_streams_and_graphs():
     second = b.recurrence_forward(x, log_a, h0=want[1])
     assert torch.equal(h, second[0]) and torch.equal(state, second[1])
     assert all(torch.equal(p, q) for p, q in zip(back, b.recurrence_backward(log_a, h, x, h0=h0, dhT=dhT)))
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("B,T,C", [(1, 12, 64), (300, 40, 132), (1, 300, 63), (2, 500, 64), (1, 1500, 2304), (1, 4101, 72), (1, 9000, 8), (1, 3000, 520),
+                                   (130, 600, 64), (3, 700, 1608)])
+@pytest.mark.parametrize("decay", [-2.0, -12.0, -60.0, -100.0])
+def test_open_gates_forget_nothing_that_is_not_finite(decay, B, T, C, types):
+    """Products of open gates are zero in fp32 behind a few tokens; only a closed gate ends what is not finite, wherever the pieces of a
+    sequence meet, and a gate that is NaN is as if it were open."""
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, 31)
+    log_a.fill_(decay)
+    closed, bad = T // 3, 3 * T // 4
+    log_a[:, closed] = -math.inf
+    H, _ = b.recurrence_forward(x, log_a, h0=h0)
+    assert bool(torch.isfinite(H).all())
+    wrong, start = x.clone(), h0.clone()
+    wrong[:, bad, ::2] = math.nan
+    wrong[:, bad, 1::2] = math.inf
+    start[:, ::2] = -math.inf
+    start[:, 1::2] = math.nan
+    K, hT = b.recurrence_forward(wrong, log_a, h0=start)
+    assert not bool(torch.isfinite(K[:, :closed]).any()) and not bool(torch.isfinite(K[:, bad:]).any()) and not bool(torch.isfinite(hT).any())
+    assert torch.equal(K[:, closed:bad], H[:, closed:bad])
+    assert bool((K[:, bad:, 1::2] == math.inf).all()) and bool((K[:, :closed, ::2] == -math.inf).all())
+    # a NaN among the gates, and the closed one behind it
+    odd = log_a.clone()
+    odd[:, closed // 2] = math.nan
+    K, _ = b.recurrence_forward(x, odd, h0=h0)
+    assert bool(torch.isnan(K[:, closed // 2:closed]).all()) and torch.equal(K[:, :closed // 2], H[:, :closed // 2]) and torch.equal(K[:, closed:], H[:, closed:])
+    # gradients: from the last token to the first
+    dH = torch.randn(B, T, C, generator=g, device=DEV).to(types[0])
+    one = torch.ones_like(H)
+    dX, dA, d0 = b.recurrence_backward(log_a, one, dH, h0=h0, dhT=dhT)
+    assert bool(torch.isfinite(dX).all())
+    wrong, end = dH.clone(), dhT.clone()
+    wrong[:, closed // 2, ::2] = math.nan
+    wrong[:, closed // 2, 1::2] = math.inf
+    end[:, ::2] = math.inf
+    end[:, 1::2] = math.nan
+    eX, eA, e0 = b.recurrence_backward(log_a, one, wrong, h0=h0, dhT=end)
+    for k in (eX, eA):
+        assert not bool(torch.isfinite(k[:, :closed // 2 + 1]).any()) and not bool(torch.isfinite(k[:, closed + 1:]).any())
+    assert not bool(torch.isfinite(e0).any()) and not bool(torch.isfinite(eX[:, closed]).any()) and bool((eA[:, closed] == 0).all())
+    assert torch.equal(eX[:, closed // 2 + 1:closed], dX[:, closed // 2 + 1:closed]) and torch.equal(eA[:, closed // 2 + 1:closed], dA[:, closed // 2 + 1:closed])
