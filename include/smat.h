@@ -477,7 +477,7 @@ smat_status smat_norm_backward(const smat_norm_problem* problem, const smat_rows
  * that are not finite among it: with one at the first token of every sequence, packed sequences do not see one another.  Open
  * gates forget nothing that is not finite, however small their product.  (A gate that is zero in fp32, log_a below -104, is a closed one.)
  * The state is fp32.  h may be x.  (Kernels of long sequences wait for copies and for one another within a cluster; a wait that ran
- * out, after two seconds, leaves NaN in what follows.)
+ * out, after two seconds, leaves the tokens of its tile undefined and NaN in what follows.)
  * Backward: from dh (and dhT, the gradient at hT, NULL: none) and the h that was kept,
  *     c_t = exp(log_a_t) (dh_t + c_{t+1}),  c_T = dhT;    dx_t = dh_t + c_{t+1},  dlog_a_t = c_t h_{t-1},  dh0 = c_0
  * dx like x (may be dh), dlog_a like log_a (may be log_a), dh0 fp32 (NULL: not wanted; may be dhT).

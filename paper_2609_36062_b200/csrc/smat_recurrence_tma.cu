@@ -36,7 +36,11 @@ struct Tile {
   static constexpr uint32_t A_AT = X, H_AT = X + A;
 };
 
-// Gives up after about two seconds.  What follows from a tile that has not come is NaN; `lost` keeps later waits short.
+// Waits are given up after about two seconds.  `lost` keeps a thread's later waits short, and what follows is NaN: a tile that has not
+// come has the map of NaN, and states whose maps have not come are NaN.  A CTA in which a thread has given up (`gave_up`, read behind the round's
+// barrier) asks for no more tiles and sends no more maps, for a barrier whose phase is open cannot be armed again and the others may
+// still read the buffer that the next maps go to; so the others give up too.  At the end the cluster meets: no CTA leaves while
+// another may still send to its shared memory.
 __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, bool& lost) {
   if (tc::mbar_try_wait(bar, parity)) return;
   const long long start = clock64();
@@ -145,6 +149,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   __shared__ __align__(16) float entering[2][GROUPS][COLS];         // the state that enters a group's tokens
   __shared__ __align__(8) float2 tile_map[2][REC_MAX_CLUSTER][COLS];
   __shared__ uint64_t full[STAGES], maps_in[2];
+  __shared__ volatile int gave_up;
   const cg::cluster_group cluster = cg::this_cluster();
   const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int tid = threadIdx.x, lane = tid % (COLS / VEC), group = tid / (COLS / VEC);
@@ -156,6 +161,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     tc::mbar_init(&maps_in[0], 1);
     tc::mbar_init(&maps_in[1], 1);
     tc::fence_barrier_init();
+    gave_up = 0;
   }
   if (ranks > 1) cluster.sync();      // all of the cluster run, with their barriers ready, before one sends to another
   else __syncthreads();
@@ -164,8 +170,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   // this CTA's tile of a round is number round * ranks + rank in the order of the recurrence; the last round may have none for it
   const int own_rounds = (tiles - rank + ranks - 1) / ranks;
   const auto token_of = [&](int round) { return (BACK ? tiles - 1 - (round * ranks + rank) : round * ranks + rank) * Shape::TOKENS; };
+  int asked = 0;      // of the thread that issues copies: tiles so far
   const auto fetch = [&](int round) {
     if (round >= own_rounds) return;
+    asked = round + 1;
     char* to = stages + (round % STAGES) * Shape::BYTES;
     uint64_t* bar = &full[round % STAGES];
     const int t = token_of(round);
@@ -244,7 +252,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       const auto nothing = [](int, float2, float2) {};
       H = states(k, std::false_type(), make_float2(0.f, 0.f), nothing);
       if (rec_not_finite(fmaf(H.x, 0.f, H.y * 0.f))) H = states(k, std::true_type(), make_float2(0.f, 0.f), nothing);
-      if (lost) H = make_float2(NAN, NAN);
+      if (lost) {
+        gave_up = 1;
+        H = make_float2(NAN, NAN);
+      }
     }
     *reinterpret_cast<float4*>(&group_map[round & 1][group][lane * VEC]) = make_float4(A.x, H.x, A.y, H.y);
   };
@@ -252,13 +263,14 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
   // joined by two threads each, or by four in all warps alike, 64 K tokens took 171 and 188 us.)
   const auto publish = [&](int round) {
     if (!sends || ranks == 1) return;
-    const int turn = round & 1;
+    const int turn = round & 1, stop = gave_up;
     float2 m = group_map[turn][0][channel];
 #pragma unroll
     for (int w = 1; w < GROUPS; ++w) {
       const float2 n = group_map[turn][w][channel];
       m = make_float2(rec_joined(n.x, m.x), rec_step(n.x, m.y, n.y));
     }
+    if (stop) return;
     if (channel == 0) tc::mbar_expect_tx(&maps_in[turn], ranks * COLS * sizeof(float2));
     for (int r = 0; r < ranks; ++r) send(in_rank(&tile_map[turn][rank][channel], r), in_rank(&maps_in[turn], r), m);
   };
@@ -278,7 +290,10 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
         behind = rec_step(m.x, behind, m.y);
       }
       carry = behind;
-      if (lost) state = carry = NAN;
+      if (lost) {
+        gave_up = 1;
+        state = carry = NAN;
+      }
     }
     // (eight maps at a time ahead of the stores, which the compiler does not move them across)
 #pragma unroll
@@ -344,7 +359,7 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
       put(round - 1);
       if (round > 1) {
         asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // the outputs of round - 2 have been taken away
-        fetch(round - 2 + STAGES);
+        if (!gave_up) fetch(round - 2 + STAGES);
       }
     }
     if (round + 1 < rounds) publish(round + 1);
@@ -359,18 +374,26 @@ __global__ void __launch_bounds__(REC_THREADS, 2) recurrence_tma_kernel(const __
     step(round, even, odd);
     if (round + 1 < rounds) step(round + 1, odd, even);
   }
-  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
+  // (the barrier before the trigger: behind it CTAs of the next launch take places as those of a cluster leave one by one, and 64 K tokens
+  // of 512 channels took 57 us for 50)
+  if (ranks > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   __syncthreads();
   if (tid == PORTER) {
     put(rounds - 1);
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    // copies that were waited for in vain land before the CTA leaves, or not within the limit
-    for (int r = rounds > STAGES ? rounds - STAGES : 0; lost && r < own_rounds; ++r) {
+  }
+  if (end && rank == 0 && mine && tid < COLS) end[row + tid] = carry;
+  if (ranks > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+  pdl_trigger();      // not before: CTAs of the next launch would take places that these are laid out for
+  if (tid == PORTER && gave_up) {
+    // tiles that were waited for in vain land before the CTA leaves, or not within the limit; so do maps that the others sent before
+    // they came here (a microsecond)
+    for (int r = asked > STAGES ? asked - STAGES : 0; r < asked; ++r) {
       bool late = false;
       wait(&full[r % STAGES], (r / STAGES) & 1, late);
     }
+    for (const long long start = clock64(); clock64() - start < 1000000;) {}
   }
-  if (end && rank == 0 && mine && tid < COLS) end[row + tid] = carry;
 }
 
 template <typename TX, typename TA, int COLS, int STEPS, int STAGES, bool BACK>
