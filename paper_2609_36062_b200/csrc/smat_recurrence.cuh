@@ -3,9 +3,8 @@
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
-#include <atomic>
-
 #include "smat_launch.cuh"
+#include "smat_room.h"
 #include "smat_rows.cuh"
 
 constexpr int REC_THREADS = 256, REC_WARPS = REC_THREADS / 32, REC_MAX_CLUSTER = 8;
@@ -38,7 +37,7 @@ __device__ __forceinline__ float rec_joined(float later, float earlier) { return
 // no zero): the loops over tokens run without it, and once more with it where what they come to is not finite.
 __device__ __forceinline__ bool rec_not_finite(float zeros) { return zeros != 0.f; }
 
-// How many clusters of `ranks` CTAs of this kernel run at once on the current device; 0: not known.  (Which SMs a cluster may use is
+// How many clusters of `ranks` CTAs of this kernel run at once on the current device; -1: not known.  (Which SMs a cluster may use is
 // up to the device: of 296 places of CTAs, clusters of 8, 4 and 2 had 264, 280 and 296.)
 template <typename... KArgs>
 int rec_clusters(void (*kernel)(KArgs...), size_t smem, unsigned ranks) {
@@ -55,30 +54,23 @@ int rec_clusters(void (*kernel)(KArgs...), size_t smem, unsigned ranks) {
   int n = 0;
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess) return n;
   cudaGetLastError();
-  return 0;
+  return -1;
 }
 
-// What one kernel's rec_clusters come to, asked for once a device.
-struct RecRoom {
-  static constexpr int DEVICES = 64;
-  std::atomic<int> known[DEVICES][REC_MAX_CLUSTER + 1];      // clusters + 1
+// What one kernel's rec_clusters come to.
+using RecRoom = SmatRoom<REC_MAX_CLUSTER>;
 
-  template <typename... KArgs>
-  int operator()(void (*kernel)(KArgs...), size_t smem, unsigned ranks) {
-    int device = 0;
-    if (cudaGetDevice(&device) != cudaSuccess || device >= DEVICES) return rec_clusters(kernel, smem, ranks);
-    int n = known[device][ranks].load(std::memory_order_relaxed);
-    if (n == 0) known[device][ranks].store(n = rec_clusters(kernel, smem, ranks) + 1, std::memory_order_relaxed);
-    return n - 1;
-  }
-};
-
-// CTAs of a cluster, which take tiles in turn: as many as all run at once, and no more than there are tiles.  A second wave costs as
-// much as the first (16 K tokens of 2112 bf16 channels 42 us, with one cluster of eight too many, 2176 channels, 67).
+// CTAs of a cluster, which take tiles in turn: as many as all run at once, and no more than there are tiles; one where the device does
+// not tell.  A second wave costs as much as the first (16 K tokens of 2112 bf16 channels 42 us, with one cluster of eight too many,
+// 2176 channels, 67).
 template <typename... KArgs>
 unsigned rec_ranks(RecRoom& room, void (*kernel)(KArgs...), size_t smem, int64_t columns, int64_t batch, int64_t tiles) {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) cudaGetLastError();
   unsigned ranks = REC_MAX_CLUSTER;
-  while (ranks > 1 && (ranks > tiles || columns * batch * ranks > REC_CTAS || columns * batch > room(kernel, smem, ranks))) --ranks;
+  while (ranks > 1 && (ranks > tiles || columns * batch * ranks > REC_CTAS ||
+                       columns * batch > room(device, ranks, [&] { return rec_clusters(kernel, smem, ranks); })))
+    --ranks;
   return ranks;
 }
 

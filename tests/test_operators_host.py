@@ -1,6 +1,9 @@
 """The operators around the pass on the CPU: refusals before any launch, sizes, and the formulas of the rotary frequencies."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -186,3 +189,29 @@ def test_rotary_frequencies():
                 dict(rotated=8, scaling="yarn", fast_turns=1.0, slow_turns=2.0), dict(rotated=8, scaling="yarn", trained_length=0)):
         with pytest.raises(ValueError):
             b.rotary_frequencies(device="cpu", **bad)
+
+
+ROOM = r"""
+#include "smat_room.h"
+#include <cstdio>
+int main() {
+  static SmatRoom<8> room;
+  int asked = 0;
+  const auto says = [&](int n) { return [&asked, n] { ++asked; return n; }; };
+  // an answer that could not be had is passed on and asked for again; one that was, none among it, is kept
+  if (room(0, 8, says(-1)) != -1 || room(0, 8, says(-1)) != -1 || asked != 2) return 1;
+  if (room(0, 8, says(33)) != 33 || room(0, 8, says(-1)) != 33 || asked != 3) return 2;
+  if (room(0, 4, says(0)) != 0 || room(0, 4, says(7)) != 0 || asked != 4) return 3;
+  if (room(1, 8, says(16)) != 16 || room(0, 8, says(5)) != 33 || asked != 5) return 4;      // by device
+  if (room(64, 8, says(3)) != 3 || room(64, 8, says(4)) != 4 || room(-1, 8, says(5)) != 5 || asked != 8) return 5;      // not kept
+  std::puts("ok");
+}
+"""
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no C++ compiler")
+def test_answers_of_the_device_are_kept_only_where_there_is_one(tmp_path):
+    (tmp_path / "room.cpp").write_text(ROOM)
+    csrc = os.path.join(os.path.dirname(b.__file__), "csrc")
+    subprocess.run(["g++", "-std=c++17", f"-I{csrc}", "-o", str(tmp_path / "room"), str(tmp_path / "room.cpp")], check=True)
+    assert subprocess.run([str(tmp_path / "room")], check=True, capture_output=True, text=True).stdout == "ok\n"
