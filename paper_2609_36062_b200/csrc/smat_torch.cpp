@@ -67,14 +67,16 @@ const at::Tensor* tensor(PyObject* o, const char* name, at::ScalarType dtype, at
   return &t;
 }
 
-bool workspace(PyObject* o, const char* name, void** ptr, size_t* bytes) {
+// Memory that a call works in.  The passes and the decoding steps take what the device can reach, pinned memory of the host and strided views among
+// it (as many bytes as the tensor has elements, from its first one on); `plain`: contiguous memory of the device alone.
+bool workspace(PyObject* o, const char* name, void** ptr, size_t* bytes, bool plain) {
   if (!THPVariable_Check(o)) {
     PyErr_Format(PyExc_ValueError, "%s: expected a tensor", name);
     return false;
   }
   const at::Tensor& t = THPVariable_Unpack(o);
-  if (!t.is_cuda() || !t.is_contiguous()) {
-    PyErr_Format(PyExc_ValueError, "%s: expected a contiguous CUDA tensor", name);
+  if (plain ? !t.is_cuda() || !t.is_contiguous() : !t.is_cuda() && !t.is_pinned()) {
+    PyErr_Format(PyExc_ValueError, plain ? "%s: expected a contiguous CUDA tensor" : "%s: expected memory that the device can reach", name);
     return false;
   }
   *ptr = t.data_ptr();
@@ -177,7 +179,7 @@ PyObject* plan_forward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *ws, *st;
     size_t bytes;
     if (kind == 0 && a[5] != Py_None && !tensor(a[5], "O", p.dtype, sv)) return nullptr;
-    if (!output(a[5], "O", *V, &O) || !workspace(a[6], "workspace", &ws, &bytes) || !stream(a[7], &st)) return nullptr;
+    if (!output(a[5], "O", *V, &O) || !workspace(a[6], "workspace", &ws, &bytes, false) || !stream(a[7], &st)) return nullptr;
     const void *q = Q->data_ptr(), *k = K->data_ptr(), *v = V->data_ptr();
     void* o = O.data_ptr();
     int rc;
@@ -225,7 +227,7 @@ PyObject* plan_backward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     void *ws, *st;
     size_t bytes;
     if (!output(a[7], "dQ", *Q, &dQ) || !output(a[8], "dK", *K, &dK) || !output(a[9], "dV", *V, &dV) ||
-        (la && !output(a[10], "dlog_a", *la, &dla)) || !workspace(a[11], "workspace", &ws, &bytes) || !stream(a[12], &st))
+        (la && !output(a[10], "dlog_a", *la, &dla)) || !workspace(a[11], "workspace", &ws, &bytes, false) || !stream(a[12], &st))
       return nullptr;
     const void *q = Q->data_ptr(), *k = K->data_ptr(), *v = V->data_ptr(), *go = dO->data_ptr();
     void *gq = dQ.data_ptr(), *gk = dK.data_ptr(), *gv = dV.data_ptr();
@@ -285,7 +287,7 @@ PyObject* plan_decode_step(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     at::Tensor o;
     void *cache, *st;
     size_t bytes;
-    if (!workspace(a[5], "cache", &cache, &bytes) || !output(a[6], "o", *v, &o) || !stream(a[7], &st)) return nullptr;
+    if (!workspace(a[5], "cache", &cache, &bytes, packed) || !output(a[6], "o", *v, &o) || !stream(a[7], &st)) return nullptr;
     const void *qp = q->data_ptr(), *kp = k->data_ptr(), *vp = v->data_ptr();
     void* op = o.data_ptr();
     const float* log_a = la ? la->data_ptr<float>() : nullptr;
@@ -595,7 +597,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[12] == Py_None) {
       own = run.fresh({(int64_t)bytes}, at::kByte);
       ws = own.data_ptr();
-    } else if (!workspace(a[12], "workspace", &ws, &bytes)) {
+    } else if (!workspace(a[12], "workspace", &ws, &bytes, true)) {
       return nullptr;
     } else if (THPVariable_Unpack(a[12]).device() != H->device()) {
       PyErr_SetString(PyExc_ValueError, "workspace: on another device than H");
@@ -706,7 +708,7 @@ PyObject* plan_repack(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     const Plan& p = *reinterpret_cast<Plan*>(self);
     void *cache, *packed, *st;
     size_t bytes, packed_bytes;
-    if (!workspace(a[0], "cache", &cache, &bytes) || !workspace(a[1], "packed", &packed, &packed_bytes) || !stream(a[2], &st)) return nullptr;
+    if (!workspace(a[0], "cache", &cache, &bytes, true) || !workspace(a[1], "packed", &packed, &packed_bytes, true) || !stream(a[2], &st)) return nullptr;
     const bool packs = a[3] == Py_True;
     const int rc = unlocked([&] {
       return packs ? smat_decode_pack(p.handle, cache, bytes, packed, packed_bytes, st)

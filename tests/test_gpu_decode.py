@@ -164,3 +164,39 @@ def test_the_output_may_take_the_place_of_an_input_row(place, dtype, dk, c, gate
             b = plan.decode_step(mine["q"], mine["k"], mine["v"], t, caches[1], o=mine[place])
         assert b.data_ptr() == mine[place].data_ptr() and torch.equal(a, b), t
     assert torch.equal(caches[0], caches[1])
+
+
+@pytest.mark.parametrize("where", ["pinned", "strided"])
+def test_caches_that_the_device_can_reach(where):
+    """A cache in pinned memory of the host, or the bytes behind the first one of a strided view: steps as on one of the device."""
+    w = synth.Workload("reach", 2, 1, 2, 512, 64, 64, 64, "f32", "scaled", 9)
+    _, dev = device_inputs(w)
+    plan = binding.SmatPlan(1, 2, 512, 64, 64, 2, 64, "f32")
+    one = plan.decode_cache()
+    plan.decode_begin(dev["k"], dev["v"], one)
+    if where == "pinned":
+        other = one.cpu().pin_memory()
+        behind = other
+    else:
+        wide = torch.zeros(2 * one.numel(), dtype=torch.uint8, device="cuda")
+        behind, other = wide[:one.numel()], wide[::2]
+        behind.copy_(one)
+    n = plan.geometry().n
+    for t in range(n, n + 8):
+        row = [dev[x][:, :, t].contiguous() for x in "qkv"]
+        assert torch.equal(plan.decode_step(*row, t, one), plan.decode_step(*row, t, other)), t
+    torch.cuda.synchronize()
+    assert torch.equal(one.cpu(), behind.cpu())
+    with pytest.raises(ValueError):
+        plan.decode_step(*row, n, one.cpu())
+
+
+def test_workspace_of_a_strided_view():
+    w = synth.Workload("reach", 2, 1, 2, 512, 64, 64, 64, "f32", "scaled", 9)
+    _, dev = device_inputs(w)
+    plan = binding.SmatPlan(1, 2, 512, 64, 64, 2, 64, "f32")
+    want = plan.forward(dev["q"], dev["k"], dev["v"])
+    wide = torch.zeros(2 * plan.workspace_bytes(), dtype=torch.uint8, device="cuda")
+    assert torch.equal(want, plan.forward(dev["q"], dev["k"], dev["v"], workspace=wide[::2]))
+    with pytest.raises(ValueError):
+        plan.forward(dev["q"], dev["k"], dev["v"], workspace=wide.cpu())
