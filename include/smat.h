@@ -403,7 +403,8 @@ smat_status smat_decode_step_packed(const smat_plan* plan, const void* q, const 
  * They need no plan.  Their tensors are rows of contiguous features at any stride, so that they read what a projection
  * left and write what the pass takes (or the other way round) without a copy between.  Inputs may be broadcast (stride 0).  An output
  * is refused (SMAT_ERR_SHAPE) where its rows overlap one another.  Pointers need the alignment of their elements; rows whose
- * pointers, strides and widths are whole multiples of 16 bytes move in 16-byte pieces, others an element at a time.
+ * pointers, strides and widths are whole multiples of 16 bytes move in 16-byte pieces, others four channels (the recurrence) or two
+ * elements (rotary, bf16 norms) at a time where all of a call's rows allow it, else one.
  * Device memory of an output may be that of an input where stated (same pointer, same strides), and must not overlap one
  * otherwise.  The calls launch on the given stream of the current device and return without synchronising; they keep no
  * state, and calls on several streams may run at the same time. */

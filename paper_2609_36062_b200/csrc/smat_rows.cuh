@@ -87,9 +87,6 @@ inline bool rows_at_multiples(const smat_rows* r, smat_dtype t, int64_t batch, i
   if (tokens > 1) bits |= (uint64_t)(r->token * e);
   return (bits & (bytes - 1)) == 0;
 }
-inline bool rows_in_16(const smat_rows* r, smat_dtype t, int64_t batch, int64_t heads, int64_t tokens) {
-  return rows_at_multiples(r, t, batch, heads, tokens, 16);
-}
 
 inline bool rows_misaligned(const smat_rows* r, smat_dtype t) {
   return r && (reinterpret_cast<uintptr_t>(r->data) & (uintptr_t)(dtype_bytes(t) - 1)) != 0;
