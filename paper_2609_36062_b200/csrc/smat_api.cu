@@ -1643,6 +1643,7 @@ smat_status smat_decode_step_packed(const smat_plan* pl, const void* q, const vo
   if (!device_ok()) return SMAT_ERR_ARCH;
   const PackedCache c = packed_cache(pl, packed);
   const cudaError_t err = smat_launch_decode_step_packed(q, k, v, o, reinterpret_cast<float*>(c.tail), c.codes, c.units,
+                                                         decode_table_plan(pl)->u_bf16 ? 1 : 0,
                                                          pl->dtype == SMAT_BF16 ? 1 : 0, smat_type_of(pl->geo, t), pl->geo.B, pl->r,
                                                          pl->p, pl->bh, static_cast<cudaStream_t>(cuda_stream), log_a_t,
                                                          gated ? reinterpret_cast<float*>(c.tail + decode_state_bytes(pl)) : nullptr);

@@ -57,7 +57,8 @@ __device__ __forceinline__ float4 load_state4<int8_t>(const int8_t* p) {
 // one row of shared memory per warp (no atomics: the sum's order is fixed).  Bound by the 84 MB a step of 512 heads
 // moves: 14.6 us (12.8 at the HBM rate; 15.7 without the prefetch), where one CTA per head with one row pass in flight at
 // a time took 22.1.
-// Packed type table (TU = int8_t): the unit of a row joins its gate factor, u = (g unit) code.
+// Packed type table (TU = int8_t): the unit of a row joins its gate factor, u = (g unit) code, but for units so large that a code's value may
+// pass the table type's largest number, `most`.
 constexpr int DEC_COLS = 32, DEC_ROWS = 32, DEC_THREADS = 256;
 
 // TOGETHER: the CTAs of a head are a cluster and none writes o or the running gate before all have read q, k and it (gated
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
                                                           const T* v, T* o,
                                                           float* S, const TU* U, int64_t type,
                                                           int64_t types, int p, const float* log_a,
-                                                          float* log_g, const float* units) {
+                                                          float* log_g, const float* units, float most) {
   constexpr int r = PASSES * DEC_ROWS;
   __shared__ float part[DEC_THREADS / 32][DEC_COLS];
   pdl_trigger();
@@ -105,7 +106,15 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
     s[n].x = fmaf(ki[n], v0, a * s[n].x); s[n].y = fmaf(ki[n], v1, a * s[n].y);
     s[n].z = fmaf(ki[n], v2, a * s[n].z); s[n].w = fmaf(ki[n], v3, a * s[n].w);
     *reinterpret_cast<float4*>(Sh + (int64_t)(n * DEC_ROWS + i0) * p) = s[n];     // S_t = a_t S_{t-1} + k vᵀ
-    const float f = sizeof(TU) == 1 ? g * unit[n] : g;
+    float f = g;
+    if (sizeof(TU) == 1) {
+      f = g * unit[n];
+      if (unit[n] > 0x1p120f) {
+        const auto value = [&](float code) { return fminf(fmaxf(code * unit[n], -most), most); };
+        u[n] = make_float4(value(u[n].x), value(u[n].y), value(u[n].z), value(u[n].w));
+        f = g;
+      }
+    }
     o4[0] = fmaf(qi[n], fmaf(f, u[n].x, s[n].x), o4[0]); o4[1] = fmaf(qi[n], fmaf(f, u[n].y, s[n].y), o4[1]);
     o4[2] = fmaf(qi[n], fmaf(f, u[n].z, s[n].z), o4[2]); o4[3] = fmaf(qi[n], fmaf(f, u[n].w, s[n].w), o4[3]);
   }
@@ -130,7 +139,7 @@ __global__ void __launch_bounds__(DEC_THREADS) decode_step_kernel(const T* q, co
 template <typename T, typename TU>
 cudaError_t launch_step(const void* q, const void* k, const void* v, void* o, float* S, const void* U, int64_t type,
                         int64_t types, int r, int p, int bh, cudaStream_t st, const float* log_a, float* log_g,
-                        const float* units = nullptr) {
+                        const float* units = nullptr, float most = 0.f) {
   const unsigned slices = (unsigned)(p / DEC_COLS);
   // o in the place of q or k (o in the place of v needs nothing: a CTA reads just the columns that it writes)
   const size_t in = (size_t)bh * r * sizeof(T), out = (size_t)bh * p * sizeof(T);
@@ -139,7 +148,7 @@ cudaError_t launch_step(const void* q, const void* k, const void* v, void* o, fl
                         : (together ? decode_step_kernel<T, TU, 4, true> : decode_step_kernel<T, TU, 4, false>);
   return smat_launch_pdl_cluster(kernel, dim3(slices, (unsigned)bh), DEC_THREADS, 0, together ? slices : 1u, st,
                                  static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
-                                 static_cast<T*>(o), S, static_cast<const TU*>(U), type, types, p, log_a, log_g, units);
+                                 static_cast<T*>(o), S, static_cast<const TU*>(U), type, types, p, log_a, log_g, units, most);
 }
 
 }  // namespace
@@ -156,11 +165,12 @@ cudaError_t smat_launch_decode_step(const void* q, const void* k, const void* v,
                 : launch_step<__nv_bfloat16, float>(q, k, v, o, S, U, type, types, r, p, bh, st, log_a, log_g);
 }
 
-// The same on a packed type table: codes [bh][types][r][p] int8 and units [bh][types][r].
+// The same on a packed type table: codes [bh][types][r][p] int8 and units [bh][types][r], of a table of fp32 or bf16.
 cudaError_t smat_launch_decode_step_packed(const void* q, const void* k, const void* v, void* o, float* S, const void* codes,
-                                           const float* units, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
+                                           const float* units, int table_bf16, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
                                            cudaStream_t st, const float* log_a, float* log_g) {
   if ((r != 64 && r != 128) || (p != 64 && p != 128)) return cudaErrorInvalidValue;
-  return in_bf16 ? launch_step<__nv_bfloat16, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units)
-                 : launch_step<float, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units);
+  const float most = table_bf16 ? 0x1.fep127f : 0x1.fffffep127f;
+  return in_bf16 ? launch_step<__nv_bfloat16, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units, most)
+                 : launch_step<float, int8_t>(q, k, v, o, S, codes, type, types, r, p, bh, st, log_a, log_g, units, most);
 }

@@ -224,7 +224,7 @@ cudaError_t smat_launch_decode_step(const void* q, const void* k, const void* v,
 // The same step on a packed type table (smat_decode_pack), and the packing itself: `rows` rows of p entries to int8 codes and
 // a unit each, or back (see smat_pack.cu).  `tail` bytes (a multiple of 16) behind the table are copied as they are.
 cudaError_t smat_launch_decode_step_packed(const void* q, const void* k, const void* v, void* o, float* S, const void* codes,
-                                           const float* units, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
+                                           const float* units, int table_bf16, int in_bf16, int64_t type, int64_t types, int r, int p, int bh,
                                            cudaStream_t st, const float* log_a, float* log_g);
 cudaError_t smat_launch_pack(const void* table, int table_bf16, void* codes, float* units, int64_t rows, int p, const void* tail_from,
                              void* tail_to, size_t tail, cudaStream_t st);

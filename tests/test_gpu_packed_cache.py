@@ -344,3 +344,30 @@ def test_steps_on_the_unpacked_cache(case, gated):
         bound = torch.einsum("hi,hij->hj", q, U * (value + 2.0 ** -23) + (U + v.S.double().abs()) * 2 * (w.d_k + 2) * 2.0 ** -24)
         off = (one.double() - two.double()).abs().view(bh, -1) - (half * (one.double().abs() + two.double().abs()).view(bh, -1) + bound)
         assert float(off.max()) <= 0.0, (t, float(off.max()))
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("case", [(2, 512, 64, 64, 64, "f32", 0), (2, 1024, 128, 128, 128, "bf16", 0), (2, 512, 64, 64, 32, "bf16", 0)])
+def test_steps_on_rows_at_the_end_of_the_range(case, gated):
+    """Half a unit above a row's largest entry there is no number of the type: a step reads the largest one, as unpacking does."""
+    w, _, dev, plan, la = make(case, gated)
+    cache = begin(plan, dev, la)
+    cache.zero_()
+    c = Cache(plan, cache, False)
+    most = torch.finfo(c.table.dtype).max
+    c.table[:, 1, 3], c.table[:, 1, 5, ::2], c.table[:, 1, 7], c.table[:, 1, 9, 1] = most, -most, most / 2, -most
+    packed = plan.decode_pack(cache)
+    back = Cache(plan, plan.decode_unpack(packed), False).table
+    assert bool((back[:, 1, 3] == most).all()) and bool((back[:, 1, 5, ::2] == -most).all()) and bool((back[:, 1, 9, 1] == -most).all())
+    n, (B, H, _, r, p) = plan.geometry().n, plan.shape
+    zero = torch.zeros(B, H, p, device="cuda", dtype=dev["v"].dtype)
+    for i, factor in ((3, 0.25), (5, 2.0 ** -20), (7, 1.0), (9, 0.5)):
+        q = torch.zeros(B, H, r, device="cuda", dtype=dev["q"].dtype)
+        q[..., i] = factor
+        spare = packed.clone()
+        lt = torch.full((B * H,), -math.log(2.0), device="cuda") if gated else None
+        o = plan.decode_step_packed(q, torch.zeros_like(q), zero, n, spare, log_a_t=lt)
+        want = back[:, 1, i].double().view(B, H, p) * factor * (0.5 if gated else 1.0)
+        half = torch.finfo(o.dtype).eps / 2
+        # of the table's type the value is rounded again (unpacked), of fp32 the gate's exponential and the products
+        assert bool(((o.double() - want).abs() <= want.abs() * (half + (2.0 ** -8 if c.table.dtype == torch.bfloat16 else 0.0) + 2.0 ** -21)).all()), i
