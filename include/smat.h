@@ -440,7 +440,8 @@ smat_status smat_rotary(const smat_rotary_problem* problem, const smat_rows* q, 
  *     y = h / sqrt(mean(h^2) + eps) * weight * act(gate)          (gate NULL: 1)
  * weight: DEVICE fp32 [width], or [groups, width] with weight_group = width; scale: DEVICE fp32 [width].
  * h (NULL: not kept) is stored rounded to dtype; y is formed from the unrounded rows.  h may be residual or x, y may be x or gate.
- * Sums are fp32.  1 <= width <= 16384, groups <= 65535, batch * T < 2^31.
+ * Sums are fp32: a row whose sum of squares passes fp32's largest number (entries of 10^18 and above) comes out as zeros.
+ * 1 <= width <= 16384, groups <= 65535, batch * T < 2^31.
  * Backward: from dy, the h that was kept (x itself where there is neither residual nor scale) and dh_in (the gradient that
  * reaches h by other ways, NULL: none)
  *     dh     the gradient at h, which is also that of the residual        (may be dy or dh_in)
