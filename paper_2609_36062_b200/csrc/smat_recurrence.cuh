@@ -74,7 +74,7 @@ unsigned rec_ranks(RecRoom& room, void (*kernel)(KArgs...), size_t smem, int64_t
   return ranks;
 }
 
-// The kernel whose tiles move by TMA (smat_recurrence_tma.cu), where every operand's rows are whole multiples of 16 bytes apart.
+// The kernel whose tiles move by TMA (smat_recurrence_tma.cu), where every operand's rows are whole multiples of 16 bytes, and as far apart.
 // bf16: of x, gates.
 bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back);
 cudaError_t smat_launch_recurrence_tma(const RecArgs& a, int batch, int x_bf16, int gate_bf16, bool back, cudaStream_t st);

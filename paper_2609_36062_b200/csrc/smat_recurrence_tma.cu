@@ -447,6 +447,8 @@ bool smat_recurrence_tma_supported(const RecArgs& a, int batch, int x_bf16, int 
     return (bits & 15) == 0 && s.token >= a.channels && s.token < most && (batch == 1 || (s.batch > 0 && s.batch < most));
   };
   const int x = x_bf16 ? 2 : 4, g = gate_bf16 ? 2 : 4;
+  // A store ends at a multiple of 16 bytes, not at the row's last element: rows of 13 bf16 channels, 16 apart, had zeros written behind each.
+  if (a.channels * x % 16 != 0 || (back && a.channels * g % 16 != 0)) return false;
   return fits(a.x, a.xs, x) && fits(a.log_a, a.as, g) && fits(a.out, a.os, x) && (!back || (fits(a.h, a.hs, x) && fits(a.dlog_a, a.das, g)));
 }
 

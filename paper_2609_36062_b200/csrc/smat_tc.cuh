@@ -9,7 +9,8 @@
 bool smat_make_map_2d_bf16(CUtensorMap* map, const void* base, uint64_t inner, uint64_t rows, uint32_t box_inner,
                            uint32_t box_rows, int swizzle128);
 
-// The same for rows of features at any strides (see smat_tc.cu).
+// The same for rows of features at any strides (see smat_tc.cu).  Stores through it write whole pieces of 16 bytes: `inner` has to be a
+// multiple of them.
 bool smat_make_map_rows(CUtensorMap* map, const void* base, int bytes, uint64_t inner, uint64_t rows, uint64_t batch, uint64_t row_stride,
                         uint64_t batch_stride, uint32_t box_inner, uint32_t box_rows);
 

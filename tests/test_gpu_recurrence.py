@@ -379,3 +379,29 @@ def test_open_gates_forget_nothing_that_is_not_finite(decay, B, T, C, types):
         assert not bool(torch.isfinite(k[:, :closed // 2 + 1]).any()) and not bool(torch.isfinite(k[:, closed + 1:]).any())
     assert not bool(torch.isfinite(e0).any()) and not bool(torch.isfinite(eX[:, closed]).any()) and bool((eA[:, closed] == 0).all())
     assert torch.equal(eX[:, closed // 2 + 1:closed], dX[:, closed // 2 + 1:closed]) and torch.equal(eA[:, closed // 2 + 1:closed], dA[:, closed // 2 + 1:closed])
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("B,T,C", [(6, 1023, 13), (1, 20, 100), (1, 3000, 12), (2, 300, 66), (1, 2500, 516), (3, 700, 1601), (1, 5000, 1)])
+def test_what_lies_behind_a_row_stays(B, T, C, types):
+    """Rows a multiple of 16 bytes apart, whose last element is not the last of 16 bytes: nothing behind it is written."""
+    x, log_a, h0, dhT, g = inputs(B, T, C, types, B + T + C, 100.0)
+    wide = (C // 8 + 1) * 8
+
+    def apart(v):
+        room = torch.full((B, T, wide), 5.0, dtype=v.dtype, device=DEV)
+        room[..., :C] = v
+        return room, room[..., :C]
+
+    (_, x), (_, log_a) = apart(x), apart(log_a)
+    room, H = apart(torch.zeros_like(x))
+    check_forward(x, log_a, h0, H=H)
+    assert bool((room[..., C:] == 5).all())
+    _, dH = apart(torch.randn(B, T, C, generator=g, device=DEV).to(types[0]))
+    (dx_room, dX), (da_room, dA) = apart(torch.zeros_like(x)), apart(torch.zeros_like(log_a))
+    check_backward(log_a, H, dH, h0, dhT, dX=dX, dlog_a=dA)
+    assert bool((dx_room[..., C:] == 5).all()) and bool((da_room[..., C:] == 5).all())
+    keep = x.clone()
+    room, y = apart(x)
+    again, _ = b.recurrence_forward(y, log_a, h0=h0, H=y)                       # in the place of x
+    assert torch.equal(again, H) and bool((room[..., C:] == 5).all()) and torch.equal(x, keep)
