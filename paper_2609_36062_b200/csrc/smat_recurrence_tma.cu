@@ -12,9 +12,9 @@
 // ahead, so that a round hides their way.  What sends the map of round n + 1 comes after a barrier behind all reads of those of
 // round n - 1, which lay in the same buffer, and after the maps of round n have come from all others: two buffers are enough.
 //
-// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 153 us where their
-// bytes take 122 (0.80 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 168 of 143 (0.85); without TMA, maps a
-// round ahead and pairs of channels the first took 233 us.
+// Bound by what a round issues and waits for: 64 K tokens of 2048 bf16 channels (256 CTAs, eight to a cluster) take 155 to 160 us, by
+// the GPU, where their bytes take 122 (0.76 to 0.79 of the measured copy rate), gradients of 4 x 8 K with fp32 gates 168 of 143 (0.85);
+// without TMA, maps a round ahead and pairs of channels the first took 233 us.
 #include <type_traits>
 
 #include "smat_recurrence.cuh"
@@ -426,11 +426,11 @@ cudaError_t narrow(const RecArgs& a, int batch, int cols, cudaStream_t st) {
 
 // Channels of a tile.  A long sequence of few channels leaves SMs idle with 64 (a line of bf16): with 32 or 16, whose rows are half and a
 // quarter of a line, a CTA has two and four times as many tokens a tile, and more CTAs run.  16 K tokens of bf16, forward and backward,
-// in us, with 64, 32, 16:   512 channels  27, 40   22, 30   16, 23        704 channels  27, 41   22, 31   19, 25
-//                          1024 channels  36, 51   24, 34   25, 34       1728 channels  39, 55   34, 46   43, 62
-//                          2048 channels  42, 59   40, 57   43, 63,
-// and 512 tokens of 512 channels 2.8, 3.6   3.3, 3.5   3.8, 3.2.  (fp32: 704 channels 57, 75   40, 49   31, 40; 2048  77, 105   69, 107
-// 75, 107.)
+// in us, with 64, 32, 16:   512 channels  29, 42   23, 32   16, 23        704 channels  29, 45   24, 34   20, 28
+//                          1024 channels  37, 54   25, 34   27, 37       1728 channels  41, 61   35, 50   45, 79
+//                          2048 channels  43, 66   42, 61   46, 79,
+// and 512 tokens of 512 channels 3.0, 3.9   2.9, 3.3   3.3, 3.5.  (fp32: 704 channels 59, 80   43, 55   33, 45; 2048  78, 117   74, 115
+// 81, 118.)
 int rec_cols(const RecArgs& a, int batch) {
   const int64_t columns = (a.channels + 63) / 64 * batch;
   return a.T < 2048 || columns > 28 ? 64 : columns > 11 ? 32 : 16;
