@@ -105,3 +105,17 @@ def test_given_streams_inside_a_graph():
     for got in (one, two):
         assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
     assert torch.equal(y, b.norm_forward(want[0], w))
+
+
+@pytest.mark.parametrize("name", ["rotary", "norm_backward", "recurrence_forward", "decode_pack"])
+def test_the_default_stream_given_beside_another_current_one(name):
+    call = calls()[name]
+    want = [t.clone() for t in flat(call(None))]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = flat(call(torch.cuda.default_stream()))
+        side.wait_stream(torch.cuda.default_stream())
+        assert torch.cuda.current_stream() == side
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    torch.cuda.synchronize()
